@@ -526,8 +526,125 @@ SFDA_API int sfda_backward_withheld_handoff(const void *q, const void *k, const 
                            int B, int T, int H, int d_k, int d_v, int dtype, unsigned wait_ticks,
                            void *workspace, size_t workspace_bytes, void *stream);
 
-/* Number of kernels the last sfda_forward* / sfda_step / sfda_chunk_factors / sfda_frontend call of
- * this thread enqueued (host only; for launch accounting in benchmarks). */
+/*
+ * Linear attention with a fixed decay for each head: the recurrence without rotations and without the erase term, for
+ * layers that stand beside those of Eq. "sfda" in a hybrid stack (its decay is one constant of the head, nothing is
+ * learned per token):
+ *
+ *     S_t = gamma_h S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t,   gamma_h = exp(log_decay[h]).
+ *
+ *  q [B][T][H][d_k] dtype     k [B][T][H_kv][d_k] dtype     v [B][T][H_kv][d_v] dtype
+ *         H_kv divides H; query head h reads key and value head h / (H / H_kv).
+ *  log_decay [H] float: <= 0 is a precondition that is not checked; 0 never forgets, -infinity keeps the token alone.
+ *  lens   [B] int32 (device), or NULL for T everywhere: the number of tokens of each sequence, taken as 0 or T where it lies
+ *         outside [0, T].  Rows of q, k, v behind a sequence's end are not used, rows of o (and of gradients) behind it
+ *         are left as they were; the final state is that after the last token, of a sequence of no tokens S0.
+ *  S0     [B][H][d_k][d_v] float, or NULL (zero)
+ *  o      [B][T][H][d_v] dtype
+ *  S_T    [B][H][d_k][d_v] float, or NULL; may alias S0
+ *  workspace: sfda_linear_workspace_bytes(...) bytes of device scratch (NULL when that is 0), 16-byte aligned, clobbered;
+ *         calls whose work may overlap on the GPU need one each.
+ *
+ * d_k, d_v in {64, 128}; any H, B and T >= 1.  SFDA_ERR_SHAPE where H_kv does not divide H, SFDA_ERR_VALUE for a scale that
+ * is not finite.  The state and all sums are fp32.  A value that is not finite makes NaN of the outputs and states that
+ * depend on it, and of nothing else.  The result is deterministic.
+ */
+SFDA_API size_t sfda_linear_workspace_bytes(int B, int T, int H, int H_kv, int d_k, int d_v, int dtype);
+SFDA_API int sfda_linear_forward(const void *q, const void *k, const void *v, const float *log_decay, const int32_t *lens,
+                                 const float *S0, void *o, float *S_T,
+                                 int B, int T, int H, int H_kv, int d_k, int d_v, int dtype, float scale,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Its gradients: of a real loss, given the cotangents d_o [B][T][H][d_v] dtype of the outputs and dS_T [B][H][d_k][d_v]
+ * float of the final state (or NULL: zero).  With G_t = gamma_h G_{t+1} + scale q_t d_o_t^T and G behind the last token
+ * = dS_T:  dq_t = scale S_t d_o_t,  dk_t = G_t v_t,  dv_t = G_t^T k_t,  dS0 = gamma_h G_1.
+ *
+ *  dq [B][T][H][d_k], dk [B][T][H_kv][d_k], dv [B][T][H_kv][d_v] dtype (those of shared heads are sums over the query heads
+ *  that read them, added in fp32 in a fixed order and rounded once);  dS0 [B][H][d_k][d_v] float.  All four are required
+ *  and overwritten; dS0 must not alias dS_T (SFDA_ERR_VALUE).  log_decay is a constant: it has no gradient.
+ *  workspace: sfda_linear_backward_workspace_bytes(...) bytes.  Everything else as sfda_linear_forward.
+ */
+SFDA_API size_t sfda_linear_backward_workspace_bytes(int B, int T, int H, int H_kv, int d_k, int d_v, int dtype);
+SFDA_API int sfda_linear_backward(const void *q, const void *k, const void *v, const float *log_decay, const int32_t *lens,
+                                  const float *S0, const void *d_o, const float *dS_T,
+                                  void *dq, void *dk, void *dv, float *dS0,
+                                  int B, int T, int H, int H_kv, int d_k, int d_v, int dtype, float scale,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One token of it for B * H independent states, updating S [B][H][d_k][d_v] float in place:
+ *  q [B][H][d_k], k [B][H_kv][d_k], v [B][H_kv][d_v] dtype, log_decay [H] float, o [B][H][d_v] dtype.
+ */
+SFDA_API int sfda_linear_step(const void *q, const void *k, const void *v, const float *log_decay, float *S, void *o,
+                              int B, int H, int H_kv, int d_k, int d_v, int dtype, float scale, void *stream);
+
+/*
+ * Rotary positions: the first `rot` channels of every head of q (and k), as rot / 2 pairs, each turned by the angle
+ * position * frequency and multiplied by `amplitude`; the other channels are copied.
+ *
+ *  q, q_out  rows of [H][d] dtype     k, k_out  rows of [H_kv][d] dtype, or both NULL (H_kv is then ignored)
+ *         One row per token, B * T of them, *_stride elements from one to the next (heads are dense within a row): a slice of
+ *         a packed projection works.  An output may be its own input (with the same stride); other overlaps may not.
+ *  positions [B * T] int32: any value, negative ones too
+ *  turns     [rot / 2] uint64: the frequency of each pair in 2^-64 turns per position (sfda_rotary_turns).  position * turns,
+ *         modulo 2^64, is the exact angle within the turn however far the position is; its upper 32 bits are used.
+ *  layout    SFDA_ROTARY_PAIRS: channels 2j, 2j + 1 are a pair (as the keys' complex coordinates elsewhere in this library);
+ *            SFDA_ROTARY_HALVES: channels j, j + rot / 2
+ *  inverse   != 0: turned the other way (times amplitude as well): the gradient with respect to q, k from that to q_out, k_out
+ *
+ * d even, 2 <= d <= 1024; rot even, 0 <= rot <= d; strides even and at least a row's elements (SFDA_ERR_SHAPE otherwise);
+ * SFDA_ERR_VALUE for an unknown layout or an amplitude that is not finite.  fp32 arithmetic, one rounding at the end.
+ */
+typedef enum { SFDA_ROTARY_PAIRS = 0, SFDA_ROTARY_HALVES = 1 } sfda_rotary_layout;
+SFDA_API int sfda_rotary(const void *q, const void *k, const int32_t *positions, const uint64_t *turns, void *q_out, void *k_out,
+                         int B, int T, int H, int H_kv, int d, int rot, int64_t q_stride, int64_t k_stride,
+                         int64_t q_out_stride, int64_t k_out_stride, int layout, float amplitude, int inverse, int dtype,
+                         void *stream);
+
+/*
+ * The frequencies of sfda_rotary (host only): turns[j] = rint(f_j / (2 pi) 2^64) for j < rot / 2, with
+ * f_j = base^(-2j / rot), scaled for contexts `factor` (>= 1) times the trained one:
+ *  SFDA_ROTARY_PLAIN   f_j as it is (factor is ignored)
+ *  SFDA_ROTARY_LINEAR  f_j / factor
+ *  SFDA_ROTARY_BASE    the base times factor^(rot / (rot - 2)): the last pair slows by factor, the first not at all
+ *                      (rot > 2)
+ *  SFDA_ROTARY_PARTS   s f_j + (1 - s) f_j / factor with s = (trained f_j / (2 pi) - low) / (high - low) kept in [0, 1]: pairs
+ *                      that turn more than `high` times within `trained` positions stay, those below `low` slow by factor
+ * SFDA_ERR_SHAPE for rot < 2 or odd, SFDA_ERR_VALUE for base <= 1, factor < 1, high <= low, trained <= 0 or an unknown scaling.
+ */
+typedef enum { SFDA_ROTARY_PLAIN = 0, SFDA_ROTARY_LINEAR = 1, SFDA_ROTARY_BASE = 2, SFDA_ROTARY_PARTS = 3 } sfda_rotary_scaling;
+SFDA_API int sfda_rotary_turns(uint64_t *turns, int rot, double base, int scaling, double factor, double low, double high,
+                               double trained);
+
+/*
+ * Group norm, channels last, with an activation or a gate: every row's C channels in G groups of C / G (a head each, after
+ * attention), each normalised by itself,
+ *
+ *     n = (x - mean) / sqrt(var + eps),   z = n weight + bias,   y = act(z)   or, with a gate,   y = z act(gate),
+ *
+ *  x, gate, y [rows][C] dtype (gate may be NULL)     weight, bias [C] float, or NULL (1 and 0)
+ *  act       SFDA_ACT_NONE: the identity; SFDA_ACT_SILU: u / (1 + exp(-u))
+ *  y may be x or gate.  mean and var (divided by C / G) are those of the row's group alone, so rows are independent: tokens of
+ *  a causal model.  Any G that divides C; at most 65535 groups wider than 128 accesses of 16 bytes (8 of 4 bytes where C / G
+ *  is not a multiple of 4).  SFDA_ERR_VALUE unless eps is positive and finite.
+ *
+ * sfda_group_norm_backward: the gradients from dy [rows][C] dtype:  dx, dgate [rows][C] dtype (dgate is required with a
+ * gate and ignored without), dweight, dbias [C] float, either of which may be NULL.  dx may be dy, dgate may be gate.
+ * workspace: sfda_group_norm_backward_workspace_bytes(rows, C) bytes where dweight or dbias is wanted (may be NULL
+ * otherwise); clobbered.  The sums over rows are taken in a fixed order.
+ */
+typedef enum { SFDA_ACT_NONE = 0, SFDA_ACT_SILU = 1 } sfda_act;
+SFDA_API int sfda_group_norm(const void *x, const float *weight, const float *bias, const void *gate, void *y,
+                             int64_t rows, int C, int G, float eps, int act, int dtype, void *stream);
+SFDA_API size_t sfda_group_norm_backward_workspace_bytes(int64_t rows, int C);
+SFDA_API int sfda_group_norm_backward(const void *x, const float *weight, const float *bias, const void *gate, const void *dy,
+                                      void *dx, float *dweight, float *dbias, void *dgate,
+                                      int64_t rows, int C, int G, float eps, int act, int dtype,
+                                      void *workspace, size_t workspace_bytes, void *stream);
+
+/* Number of kernels the last sfda_forward* / sfda_step / sfda_chunk_factors / sfda_frontend / sfda_linear_* /
+ * sfda_rotary / sfda_group_norm* call of this thread enqueued (host only; for launch accounting in benchmarks). */
 SFDA_API int sfda_last_launch_count(void);
 
 #ifdef __cplusplus

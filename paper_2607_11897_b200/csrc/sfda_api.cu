@@ -1,9 +1,12 @@
 // C ABI of the library: argument validation on the host, dispatch to the kernels.
 #include "../../include/sfda.h"
 
+#include <math.h>
+
 #include <mutex>
 
 #include "sfda_internal.h"
+#include "sfda_linear.h"
 
 namespace {
 
@@ -155,6 +158,29 @@ int step_common(const void *q, const void *k, const void *v, const float *alpha,
                                                                                                     : SFDA_ERR_CUDA;
 }
 
+int check_linear(int B, int T, int H, int H_kv, int d_k, int d_v, int dtype)
+{
+    if (B < 1 || T < 1 || H < 1 || H_kv < 1 || H % H_kv != 0) return SFDA_ERR_SHAPE;
+    return check_dims(d_k, d_v, 64, dtype);
+}
+template <size_t N>
+int check_aligned(const void *const (&ptrs)[N])
+{
+    for (const void *p : ptrs)
+        if (p && !aligned16(p)) return SFDA_ERR_ALIGN;
+    return SFDA_OK;
+}
+int status_of(cudaError_t e) { return e == cudaSuccess ? SFDA_OK : SFDA_ERR_CUDA; }
+
+int check_norm(const void *x, int64_t rows, int C, int G, float eps, int act, int dtype)
+{
+    if (!x) return SFDA_ERR_NULL;
+    if (rows < 1 || C < 1 || G < 1 || C % G != 0) return SFDA_ERR_SHAPE;
+    if (dtype != SFDA_F32 && dtype != SFDA_BF16) return SFDA_ERR_UNSUPPORTED;
+    if (!sfda::group_norm_supported(C, G, dtype)) return SFDA_ERR_UNSUPPORTED;
+    return eps > 0.f && isfinite(eps) && (act == SFDA_ACT_NONE || act == SFDA_ACT_SILU) ? SFDA_OK : SFDA_ERR_VALUE;
+}
+
 }  // namespace
 
 extern "C" {
@@ -170,7 +196,7 @@ const char *sfda_status_string(int status)
         case SFDA_ERR_WORKSPACE: return "workspace missing or too small";
         case SFDA_ERR_CUDA: return "CUDA runtime error at launch";
         case SFDA_ERR_TIMEOUT: return "a bounded device-side wait ran out";
-        case SFDA_ERR_VALUE: return "a scalar of the stable parameterisation is out of range";
+        case SFDA_ERR_VALUE: return "a scalar argument is out of range";
         default: return "unknown status";
     }
 }
@@ -730,6 +756,148 @@ int sfda_backward_withheld_handoff(const void *q, const void *k, const void *v, 
 {
     return backward_common(q, k, v, alpha, theta, beta, S0, d_o, d_o_im, dS_T, dq, dk, dv, dalpha, dtheta, dbeta, dS0, B,
                            T, H, d_k, d_v, dtype, true, wait_ticks, workspace, workspace_bytes, stream);
+}
+
+// ---- linear attention with a fixed decay for each head, rotary positions, group norm ---------------------
+size_t sfda_linear_workspace_bytes(int B, int T, int H, int H_kv, int d_k, int d_v, int dtype)
+{
+    if (check_linear(B, T, H, H_kv, d_k, d_v, dtype) != SFDA_OK) return 0;
+    return sfda::linear_forward_bytes({nullptr, nullptr, B, T, H, dtype}, d_k, d_v);
+}
+
+int sfda_linear_forward(const void *q, const void *k, const void *v, const float *log_decay, const int32_t *lens, const float *S0,
+                        void *o, float *S_T, int B, int T, int H, int H_kv, int d_k, int d_v, int dtype, float scale,
+                        void *workspace, size_t workspace_bytes, void *stream)
+{
+    g_last_launches = 0;
+    if (!q || !k || !v || !log_decay || !o) return SFDA_ERR_NULL;
+    int rc = check_linear(B, T, H, H_kv, d_k, d_v, dtype);
+    if (rc != SFDA_OK) return rc;
+    if (!isfinite(scale)) return SFDA_ERR_VALUE;
+    if ((rc = check_aligned({q, k, v, log_decay, lens, S0, o, S_T, workspace})) != SFDA_OK) return rc;
+    const sfda::LinearArgs a = {log_decay, lens, B, T, H, dtype};
+    const size_t need = sfda::linear_forward_bytes(a, d_k, d_v);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return SFDA_ERR_WORKSPACE;
+    return status_of(sfda::launch_linear_forward(a, q, k, v, S0, o, S_T, H_kv, d_k, d_v, scale, workspace,
+                                                 static_cast<cudaStream_t>(stream), &g_last_launches));
+}
+
+size_t sfda_linear_backward_workspace_bytes(int B, int T, int H, int H_kv, int d_k, int d_v, int dtype)
+{
+    if (check_linear(B, T, H, H_kv, d_k, d_v, dtype) != SFDA_OK) return 0;
+    return sfda::linear_backward_bytes({nullptr, nullptr, B, T, H, dtype}, H_kv, d_k, d_v);
+}
+
+int sfda_linear_backward(const void *q, const void *k, const void *v, const float *log_decay, const int32_t *lens, const float *S0,
+                         const void *d_o, const float *dS_T, void *dq, void *dk, void *dv, float *dS0, int B, int T, int H,
+                         int H_kv, int d_k, int d_v, int dtype, float scale, void *workspace, size_t workspace_bytes, void *stream)
+{
+    g_last_launches = 0;
+    if (!q || !k || !v || !log_decay || !d_o || !dq || !dk || !dv || !dS0) return SFDA_ERR_NULL;
+    int rc = check_linear(B, T, H, H_kv, d_k, d_v, dtype);
+    if (rc != SFDA_OK) return rc;
+    if (!isfinite(scale) || dS0 == dS_T) return SFDA_ERR_VALUE;
+    if ((rc = check_aligned({q, k, v, log_decay, lens, S0, d_o, dS_T, dq, dk, dv, dS0, workspace})) != SFDA_OK) return rc;
+    const sfda::LinearArgs a = {log_decay, lens, B, T, H, dtype};
+    const size_t need = sfda::linear_backward_bytes(a, H_kv, d_k, d_v);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return SFDA_ERR_WORKSPACE;
+    return status_of(sfda::launch_linear_backward(a, q, k, v, S0, d_o, dS_T, dq, dk, dv, dS0, H_kv, d_k, d_v, scale, workspace,
+                                                  static_cast<cudaStream_t>(stream), &g_last_launches));
+}
+
+int sfda_linear_step(const void *q, const void *k, const void *v, const float *log_decay, float *S, void *o, int B, int H,
+                     int H_kv, int d_k, int d_v, int dtype, float scale, void *stream)
+{
+    g_last_launches = 0;
+    if (!q || !k || !v || !log_decay || !S || !o) return SFDA_ERR_NULL;
+    int rc = check_linear(B, 1, H, H_kv, d_k, d_v, dtype);
+    if (rc != SFDA_OK) return rc;
+    if (!isfinite(scale)) return SFDA_ERR_VALUE;
+    if ((rc = check_aligned({q, k, v, log_decay, S, o})) != SFDA_OK) return rc;
+    return status_of(sfda::launch_linear_step({q, k, v, log_decay, S, o, B, H, H_kv, d_k, d_v, dtype, scale},
+                                              static_cast<cudaStream_t>(stream), &g_last_launches));
+}
+
+int sfda_rotary(const void *q, const void *k, const int32_t *positions, const uint64_t *turns, void *q_out, void *k_out, int B,
+                int T, int H, int H_kv, int d, int rot, int64_t q_stride, int64_t k_stride, int64_t q_out_stride,
+                int64_t k_out_stride, int layout, float amplitude, int inverse, int dtype, void *stream)
+{
+    g_last_launches = 0;
+    if (!q || !q_out || !k != !k_out || !positions || (rot > 0 && !turns)) return SFDA_ERR_NULL;
+    if (!k) H_kv = 0, k_stride = k_out_stride = 0;
+    if (B < 1 || T < 1 || H < 1 || H_kv < (k ? 1 : 0) || d < 2 || d % 2 != 0 || d > 1024 || rot < 0 || rot % 2 != 0 || rot > d)
+        return SFDA_ERR_SHAPE;
+    const int64_t strides[] = {q_stride, q_out_stride, k_stride, k_out_stride};
+    for (int i = 0; i < 4; ++i)
+        if (strides[i] < (int64_t)(i < 2 ? H : H_kv) * d || strides[i] % 2 != 0) return SFDA_ERR_SHAPE;
+    if (dtype != SFDA_F32 && dtype != SFDA_BF16) return SFDA_ERR_UNSUPPORTED;
+    if ((layout != SFDA_ROTARY_PAIRS && layout != SFDA_ROTARY_HALVES) || !isfinite(amplitude)) return SFDA_ERR_VALUE;
+    const int rc = check_aligned({q, k, static_cast<const void *>(positions), static_cast<const void *>(turns),
+                                  static_cast<const void *>(q_out), static_cast<const void *>(k_out)});
+    if (rc != SFDA_OK) return rc;
+    sfda::RotaryArgs a;
+    a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out; a.positions = positions; a.turns = turns;
+    a.rows = (long long)B * T;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.qo_stride = q_out_stride; a.ko_stride = k_out_stride;
+    a.H = H; a.H_kv = H_kv; a.d = d; a.rot = rot; a.layout = layout; a.inverse = inverse != 0; a.dtype = dtype;
+    a.amplitude = amplitude;
+    return status_of(sfda::launch_rotary(a, static_cast<cudaStream_t>(stream), &g_last_launches));
+}
+
+int sfda_rotary_turns(uint64_t *turns, int rot, double base, int scaling, double factor, double low, double high, double trained)
+{
+    if (!turns) return SFDA_ERR_NULL;
+    if (rot < 2 || rot % 2 != 0 || (scaling == SFDA_ROTARY_BASE && rot < 4)) return SFDA_ERR_SHAPE;
+    if (scaling < SFDA_ROTARY_PLAIN || scaling > SFDA_ROTARY_PARTS || !(base > 1.0) || !isfinite(base)) return SFDA_ERR_VALUE;
+    if (scaling != SFDA_ROTARY_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return SFDA_ERR_VALUE;
+    if (scaling == SFDA_ROTARY_PARTS && (!(high > low) || !(trained > 0.0) || !isfinite(high - low) || !isfinite(trained)))
+        return SFDA_ERR_VALUE;
+    const long double turn = 6.283185307179586476925286766559L;
+    long double b = base;
+    if (scaling == SFDA_ROTARY_BASE) b *= powl(factor, (long double)rot / (rot - 2));
+    for (int j = 0; j < rot / 2; ++j) {
+        long double f = powl(b, -2.0L * j / rot);
+        if (scaling == SFDA_ROTARY_LINEAR) f /= factor;
+        if (scaling == SFDA_ROTARY_PARTS) {
+            const long double s = fminl(1.0L, fmaxl(0.0L, (trained * f / turn - low) / (high - low)));
+            f = s * f + (1.0L - s) * f / factor;
+        }
+        turns[j] = (uint64_t)rintl(f / turn * 18446744073709551616.0L);
+    }
+    return SFDA_OK;
+}
+
+int sfda_group_norm(const void *x, const float *weight, const float *bias, const void *gate, void *y, int64_t rows, int C, int G,
+                    float eps, int act, int dtype, void *stream)
+{
+    g_last_launches = 0;
+    int rc = y ? check_norm(x, rows, C, G, eps, act, dtype) : SFDA_ERR_NULL;
+    if (rc != SFDA_OK || (rc = check_aligned({x, weight, bias, gate, y})) != SFDA_OK) return rc;
+    sfda::GroupNormArgs a = {};
+    a.x = x; a.gate = gate; a.weight = weight; a.bias = bias; a.y = y;
+    a.rows = rows; a.C = C; a.G = G; a.act = act; a.dtype = dtype; a.eps = eps;
+    return status_of(sfda::launch_group_norm(a, static_cast<cudaStream_t>(stream), &g_last_launches));
+}
+
+size_t sfda_group_norm_backward_workspace_bytes(int64_t rows, int C)
+{
+    return rows < 1 || C < 1 ? 0 : sfda::group_norm_backward_bytes(rows, C);
+}
+
+int sfda_group_norm_backward(const void *x, const float *weight, const float *bias, const void *gate, const void *dy, void *dx,
+                             float *dweight, float *dbias, void *dgate, int64_t rows, int C, int G, float eps, int act, int dtype,
+                             void *workspace, size_t workspace_bytes, void *stream)
+{
+    g_last_launches = 0;
+    int rc = dy && dx && (!gate || dgate) ? check_norm(x, rows, C, G, eps, act, dtype) : SFDA_ERR_NULL;
+    if (rc != SFDA_OK) return rc;
+    if ((rc = check_aligned({x, weight, bias, gate, dy, dx, dweight, dbias, dgate, workspace})) != SFDA_OK) return rc;
+    if ((dweight || dbias) && (!workspace || workspace_bytes < sfda::group_norm_backward_bytes(rows, C))) return SFDA_ERR_WORKSPACE;
+    sfda::GroupNormArgs a = {};
+    a.x = x; a.gate = gate; a.dy = dy; a.weight = weight; a.bias = bias;
+    a.dx = dx; a.dweight = dweight; a.dbias = dbias; a.dgate = gate ? dgate : nullptr;
+    a.rows = rows; a.C = C; a.G = G; a.act = act; a.dtype = dtype; a.eps = eps;
+    return status_of(sfda::launch_group_norm_backward(a, workspace, static_cast<cudaStream_t>(stream), &g_last_launches));
 }
 
 int sfda_last_launch_count(void) { return g_last_launches; }

@@ -1,0 +1,373 @@
+// sfda_group_norm: normalisation over each group of channels of a row (channels last), affine, activated or gated:
+//
+//     n = (x - mean) / sqrt(var + eps),   z = n w + b,   y = act(z)   or, with a gate,   y = z act(gate),
+//
+// and its derivative.  Bound by memory: x (gate, dy) are read once, everything between stays in registers.  A group is
+// spread over P lanes of one warp, NV accesses of V channels each; the mean is taken first and the variance from the
+// differences, both in fp32.  The differences' own mean, what the first one's rounding left, is taken off as well: where a
+// group's mean is large beside its deviation, n would otherwise be off by the mean's 2^-24 over the deviation.
+//
+// The derivative recomputes n from x (it reads the whole group anyway).  Its CTAs keep the same channels from row to row,
+// so the sums over rows behind dw and db stay in registers; each CTA writes one row of partial sums, and a second kernel
+// adds them in a fixed order.
+#include "sfda_common.cuh"
+#include "sfda_linear.h"
+#include "sfda_vec.cuh"
+
+namespace sfda {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct Dev {
+    const void *x, *gate, *dy;
+    const float *weight, *bias;
+    void *y, *dx, *dgate;
+    float *part;                 // [2][blocks over rows][C] partial sums of dw and db, or NULL
+    long long rows;
+    int C, G, D, lanes, gb, rb;  // lanes of a group; groups and rows that a CTA holds at a time
+    int silu;
+    float eps;
+};
+
+template <int V, bool kMost>
+__device__ __forceinline__ void params(const float *w, int c, float (&x)[V], float other)
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = w ? __ldg(w + c + i) : other;
+}
+
+__device__ __forceinline__ float sum_lanes(float x, int lanes)
+{
+    for (int d = lanes >> 1; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    return x;
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+
+template <typename T, int V, int NV, bool kBackward>
+__global__ void __launch_bounds__(kThreads) sfda_group_norm_kernel(const Dev p)
+{
+    const int tid = threadIdx.x, lane = tid % p.lanes, slot = tid / p.lanes;
+    // slots beyond gb * rb hold no group (but take part in the shuffles)
+    const int g0 = blockIdx.y * p.gb, grp = g0 + slot % p.gb, sub = slot / p.gb;
+    const bool have = sub < p.rb && grp < p.G;
+    const float inv = 1.f / (float)p.D;
+    float w[NV][V], b[NV][V], aw[kBackward ? NV : 1][V], ab[kBackward ? NV : 1][V];
+    bool in[NV];
+    int ch[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int e = (lane + j * p.lanes) * V;
+        in[j] = have && e < p.D;
+        ch[j] = in[j] ? grp * p.D + e : 0;
+        params<V, true>(p.weight, ch[j], w[j], 1.f);
+        params<V, true>(p.bias, ch[j], b[j], 0.f);
+        if (kBackward)
+#pragma unroll
+            for (int i = 0; i < V; ++i) aw[j][i] = ab[j][i] = 0.f;
+    }
+    const T *px = static_cast<const T *>(p.x), *pg = static_cast<const T *>(p.gate), *pd = static_cast<const T *>(p.dy);
+    const long long step = (long long)gridDim.x * p.rb;
+    for (long long base = (long long)blockIdx.x * p.rb; base < p.rows; base += step) {
+        const long long row = base + sub;
+        const bool live = have && row < p.rows;
+        float x[NV][V], gt[NV][V], dy[kBackward ? NV : 1][V];
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[j][i] = gt[j][i] = 0.f;
+            if (live && in[j]) {
+                ld_vec(px + row * p.C + ch[j], x[j]);
+                if (pg) ld_vec(pg + row * p.C + ch[j], gt[j]);
+                if constexpr (kBackward) ld_vec(pd + row * p.C + ch[j], dy[j]);
+            } else if constexpr (kBackward) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) dy[j][i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum += x[j][i];
+        const float mean = sum_lanes(sum, p.lanes) * inv;
+        float sq = 0.f, rest = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                x[j][i] = in[j] ? x[j][i] - mean : 0.f;
+                rest += x[j][i];
+                sq = fmaf(x[j][i], x[j][i], sq);
+            }
+        rest = sum_lanes(rest, p.lanes) * inv;
+        const float rstd = rsqrtf(fmaf(-rest, rest, sum_lanes(sq, p.lanes) * inv) + p.eps);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[j][i] -= in[j] ? rest : 0.f;
+        if constexpr (!kBackward) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float y[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float z = fmaf(x[j][i] * rstd, w[j][i], b[j][i]), h = pg ? gt[j][i] : z;
+                    const float a = p.silu ? h * sigmoid(h) : h;
+                    y[i] = pg ? z * a : a;
+                }
+                if (live && in[j]) st_vec(static_cast<T *>(p.y) + row * p.C + ch[j], y);
+            }
+        } else {
+            float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float dg[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float n = x[j][i] * rstd, z = fmaf(n, w[j][i], b[j][i]), h = pg ? gt[j][i] : z;
+                    const float sg = p.silu ? sigmoid(h) : 1.f;
+                    const float a = p.silu ? h * sg : h, slope = p.silu ? sg * fmaf(h, 1.f - sg, 1.f) : 1.f;
+                    const float dz = dy[j][i] * (pg ? a : slope);
+                    dg[i] = dy[j][i] * z * slope;
+                    aw[j][i] = fmaf(dz, n, aw[j][i]);
+                    ab[j][i] += dz;
+                    const float dn = dz * w[j][i];
+                    s1 += dn;
+                    s2 = fmaf(dn, n, s2);
+                    x[j][i] = n;
+                    dy[j][i] = dn;
+                }
+                if (pg && live && in[j]) st_vec(static_cast<T *>(p.dgate) + row * p.C + ch[j], dg);
+            }
+            s1 = sum_lanes(s1, p.lanes) * inv;
+            s2 = sum_lanes(s2, p.lanes) * inv;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float d[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) d[i] = rstd * (dy[j][i] - s1 - x[j][i] * s2);
+                if (live && in[j]) st_vec(static_cast<T *>(p.dx) + row * p.C + ch[j], d);
+            }
+        }
+    }
+    if constexpr (kBackward) {
+        if (!p.part) return;
+        // the rows that a CTA holds at a time end in one sum: their slots add up through shared memory, in order
+        __shared__ float red[kThreads][2 * V];
+        float *pw = p.part + (long long)blockIdx.x * p.C, *pb = pw + (long long)gridDim.x * p.C;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                red[tid][i] = aw[j][i];
+                red[tid][V + i] = ab[j][i];
+            }
+            __syncthreads();
+            if (sub == 0 && in[j]) {
+                float sw[V], sb[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) sw[i] = sb[i] = 0.f;
+                for (int r = 0; r < p.rb; ++r)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        sw[i] += red[tid + r * p.gb * p.lanes][i];
+                        sb[i] += red[tid + r * p.gb * p.lanes][V + i];
+                    }
+                st_vec(pw + ch[j], sw);
+                st_vec(pb + ch[j], sb);
+            }
+        }
+    }
+}
+
+// A group too wide for one warp's registers: one CTA per (row, group), the group read again for each step (it is in the
+// caches by then).
+__device__ float sum_block(float x, float *red)
+{
+    x = sum_lanes(x, 32);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
+    __syncthreads();
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; ++i) s += red[i];
+    return s;
+}
+template <typename T, bool kBackward>
+__global__ void __launch_bounds__(kThreads) sfda_group_norm_wide_kernel(const Dev p)
+{
+    __shared__ float red[kThreads / 32];
+    const int grp = blockIdx.y, c0 = grp * p.D;
+    const float inv = 1.f / (float)p.D;
+    const T *pg = static_cast<const T *>(p.gate);
+    float *pw = p.part ? p.part + (long long)blockIdx.x * p.C : nullptr, *pb = pw ? pw + (long long)gridDim.x * p.C : nullptr;
+    bool first = true;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, first = false) {
+        const T *x = static_cast<const T *>(p.x) + row * p.C;
+        float s = 0.f;
+        for (int c = threadIdx.x; c < p.D; c += kThreads) s += ld_val(x, c0 + c);
+        const float mean = sum_block(s, red) * inv;
+        s = 0.f;
+        float rest = 0.f;
+        for (int c = threadIdx.x; c < p.D; c += kThreads) {
+            const float d = ld_val(x, c0 + c) - mean;
+            rest += d;
+            s = fmaf(d, d, s);
+        }
+        rest = sum_block(rest, red) * inv;
+        const float rstd = rsqrtf(fmaf(-rest, rest, sum_block(s, red) * inv) + p.eps);
+        float s1 = 0.f, s2 = 0.f;
+        for (int pass = 0; pass < (kBackward ? 2 : 1); ++pass) {
+            for (int c = threadIdx.x; c < p.D; c += kThreads) {
+                const int ch = c0 + c;
+                const size_t at = (size_t)row * p.C + ch;
+                const float w = p.weight ? p.weight[ch] : 1.f, b = p.bias ? p.bias[ch] : 0.f;
+                const float n = (ld_val(x, ch) - mean - rest) * rstd, z = fmaf(n, w, b), h = pg ? ld_val(pg, at) : z;
+                const float sg = p.silu ? sigmoid(h) : 1.f, a = p.silu ? h * sg : h;
+                if (!kBackward) {
+                    st_val(static_cast<T *>(p.y), at, pg ? z * a : a);
+                    continue;
+                }
+                const float slope = p.silu ? sg * fmaf(h, 1.f - sg, 1.f) : 1.f, dy = ld_val(static_cast<const T *>(p.dy), at);
+                const float dz = dy * (pg ? a : slope), dn = dz * w;
+                if (pass == 0) {
+                    s1 += dn;
+                    s2 = fmaf(dn, n, s2);
+                    if (pw) {
+                        pw[ch] = first ? dz * n : pw[ch] + dz * n;
+                        pb[ch] = first ? dz : pb[ch] + dz;
+                    }
+                    if (pg) st_val(static_cast<T *>(p.dgate), at, dy * z * slope);
+                } else {
+                    st_val(static_cast<T *>(p.dx), at, rstd * (dn - s1 - n * s2));
+                }
+            }
+            if (kBackward && pass == 0) {
+                s1 = sum_block(s1, red) * inv;
+                s2 = sum_block(s2, red) * inv;
+            }
+        }
+    }
+}
+
+// dw, db: column sums of the partial rows, 32 columns to a CTA, eight runs of rows added in order
+__global__ void __launch_bounds__(kThreads) sfda_group_norm_sum_kernel(const float *__restrict__ part, float *dw, float *db, int n, int C)
+{
+    __shared__ float red[kThreads / 32][33];
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+    const float *src = part + (blockIdx.y ? (long long)n * C : 0);
+    float *dst = blockIdx.y ? db : dw;
+    if (!dst) return;
+    float s = 0.f;
+    if (c < C)
+        for (int r = w; r < n; r += kThreads / 32) s += src[(long long)r * C + c];
+    red[w][threadIdx.x & 31] = s;
+    __syncthreads();
+    if (w == 0 && c < C) {
+        for (int i = 1; i < kThreads / 32; ++i) s += red[i][threadIdx.x & 31];
+        dst[c] = s;
+    }
+}
+
+struct Shape {
+    int V, NV, lanes, gb, rb, blocks_y;
+    bool wide;
+};
+constexpr int kMaxNV = 4;
+
+Shape shape_of(int C, int G, int dtype)
+{
+    Shape s = {};
+    const int D = C / G;
+    s.V = dtype == 1 && D % 8 == 0 ? 8 : D % 4 == 0 ? 4 : 1;
+    const int n = D / s.V;                                  // accesses of a group
+    s.lanes = 1;
+    while (s.lanes < 32 && s.lanes < n) s.lanes *= 2;
+    s.NV = 1;
+    while (s.NV * s.lanes < n) s.NV *= 2;
+    s.wide = s.NV > kMaxNV;
+    if (s.wide) {
+        s.gb = s.rb = 1;
+        s.blocks_y = G;
+        return s;
+    }
+    const int slots = kThreads / s.lanes;
+    s.gb = G < slots ? G : slots;
+    s.rb = slots / s.gb;
+    s.blocks_y = (G + s.gb - 1) / s.gb;
+    return s;
+}
+// CTAs over the rows: a few waves of the device, so that the backward's partial sums stay few
+unsigned blocks_over_rows(const Shape &s, long long rows, int waves)
+{
+    const long long want = (rows + s.rb - 1) / s.rb, most = (148ll * waves + s.blocks_y - 1) / s.blocks_y;
+    return (unsigned)(want < most ? want : most);
+}
+constexpr int kForwardWaves = 64, kBackwardWaves = 8;
+
+template <typename T, int V, bool kBackward>
+cudaError_t launch_nv(const Shape &s, const Dev &p, dim3 grid, cudaStream_t stream)
+{
+    if (s.NV == 1) sfda_group_norm_kernel<T, V, 1, kBackward><<<grid, kThreads, 0, stream>>>(p);
+    else if (s.NV == 2) sfda_group_norm_kernel<T, V, 2, kBackward><<<grid, kThreads, 0, stream>>>(p);
+    else sfda_group_norm_kernel<T, V, 4, kBackward><<<grid, kThreads, 0, stream>>>(p);
+    return cudaGetLastError();
+}
+template <typename T, bool kBackward>
+cudaError_t launch_v(const Shape &s, const Dev &p, dim3 grid, cudaStream_t stream)
+{
+    if (s.wide) {
+        sfda_group_norm_wide_kernel<T, kBackward><<<grid, kThreads, 0, stream>>>(p);
+        return cudaGetLastError();
+    }
+    if constexpr (sizeof(T) == 2)
+        if (s.V == 8) return launch_nv<T, 8, kBackward>(s, p, grid, stream);
+    return s.V == 4 ? launch_nv<T, 4, kBackward>(s, p, grid, stream) : launch_nv<T, 1, kBackward>(s, p, grid, stream);
+}
+Dev dev_of(const GroupNormArgs &a, const Shape &s)
+{
+    return {a.x, a.gate, a.dy, a.weight, a.bias, a.y, a.dx, a.dgate, nullptr, a.rows, a.C, a.G, a.C / a.G, s.lanes, s.gb, s.rb,
+            a.act, a.eps};
+}
+
+}  // namespace
+
+bool group_norm_supported(int C, int G, int dtype) { return shape_of(C, G, dtype).blocks_y <= 65535; }
+
+cudaError_t launch_group_norm(const GroupNormArgs &a, cudaStream_t stream, int *launches)
+{
+    const Shape s = shape_of(a.C, a.G, a.dtype);
+    const dim3 grid(blocks_over_rows(s, a.rows, kForwardWaves), s.blocks_y);
+    const Dev p = dev_of(a, s);
+    const cudaError_t e = a.dtype == 1 ? launch_v<__nv_bfloat16, false>(s, p, grid, stream) : launch_v<float, false>(s, p, grid, stream);
+    if (e == cudaSuccess && launches) ++*launches;
+    return e;
+}
+
+// Over every number of groups and either dtype: a CTA row of partial sums covers all channels once.
+size_t group_norm_backward_bytes(long long rows, int C)
+{
+    const long long most = 148ll * kBackwardWaves;
+    return (size_t)(rows < most ? rows : most) * (size_t)C * 2 * sizeof(float);
+}
+
+cudaError_t launch_group_norm_backward(const GroupNormArgs &a, void *workspace, cudaStream_t stream, int *launches)
+{
+    const Shape s = shape_of(a.C, a.G, a.dtype);
+    const dim3 grid(blocks_over_rows(s, a.rows, kBackwardWaves), s.blocks_y);
+    Dev p = dev_of(a, s);
+    if (a.dweight || a.dbias) p.part = static_cast<float *>(workspace);
+    cudaError_t e = a.dtype == 1 ? launch_v<__nv_bfloat16, true>(s, p, grid, stream) : launch_v<float, true>(s, p, grid, stream);
+    if (e != cudaSuccess) return e;
+    if (launches) ++*launches;
+    if (!p.part) return cudaSuccess;
+    sfda_group_norm_sum_kernel<<<dim3((a.C + 31) / 32, 2), kThreads, 0, stream>>>(p.part, a.dweight, a.dbias, (int)grid.x, a.C);
+    e = cudaGetLastError();
+    if (e == cudaSuccess && launches) ++*launches;
+    return e;
+}
+
+}  // namespace sfda
