@@ -47,29 +47,39 @@ cudaError_t launch_sum_heads(const float *x, void *out, const LinearArgs &a, int
 }
 size_t round256(size_t x) { return (x + 255u) & ~(size_t)255u; }
 
-cudaError_t run_pass(const LinearArgs &a, const LinearPass &p, cudaStream_t stream, int *launches)
+cudaError_t run_passes(const LinearArgs &a, const LinearPass *p, int count, void *workspace, cudaStream_t stream, int *launches)
 {
-    return launch_linear_f32(a, p, stream, launches);
+    if (a.dtype == 1) return launch_linear_tc(a, p, count, workspace, stream, launches);
+    for (int i = 0; i < count; ++i) {
+        const cudaError_t e = launch_linear_f32(a, p[i], stream, launches);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+size_t pass_bytes(const LinearArgs &a, int count, int d_k, int d_v)
+{
+    return a.dtype == 1 ? round256(linear_tc_bytes(a, count, d_k, d_v)) : 0;
 }
 
 }  // namespace
 
-size_t linear_forward_bytes(const LinearArgs &, int, int) { return 0; }
+size_t linear_forward_bytes(const LinearArgs &a, int d_k, int d_v) { return pass_bytes(a, 1, d_k, d_v); }
 
 cudaError_t launch_linear_forward(const LinearArgs &a, const void *q, const void *k, const void *v, const float *S0, void *o,
-                                  float *S_T, int H_kv, int d_k, int d_v, float scale, void *, cudaStream_t stream, int *launches)
+                                  float *S_T, int H_kv, int d_k, int d_v, float scale, void *workspace, cudaStream_t stream,
+                                  int *launches)
 {
     LinearPass p = {q, k, v, o, S0, S_T, a.H, H_kv, H_kv, d_k, d_v};
     p.sp = p.se = scale;
     p.sw = 1.f;
-    return run_pass(a, p, stream, launches);
+    return run_passes(a, &p, 1, workspace, stream, launches);
 }
 
-// shared heads: the gradients of every query head in fp32, before their sums
+// the passes' scratch; with shared heads also the gradients of every query head in fp32, before their sums
 size_t linear_backward_bytes(const LinearArgs &a, int H_kv, int d_k, int d_v)
 {
     const size_t rows = (size_t)a.B * a.T * a.H;
-    return H_kv == a.H ? 0 : round256(rows * d_k * 4) + round256(rows * d_v * 4);
+    return pass_bytes(a, 3, d_k, d_v) + (H_kv == a.H ? 0 : round256(rows * d_k * 4) + round256(rows * d_v * 4));
 }
 
 cudaError_t launch_linear_backward(const LinearArgs &a, const void *q, const void *k, const void *v, const float *S0,
@@ -77,29 +87,25 @@ cudaError_t launch_linear_backward(const LinearArgs &a, const void *q, const voi
                                    int d_k, int d_v, float scale, void *workspace, cudaStream_t stream, int *launches)
 {
     const bool shared = H_kv != a.H;
-    float *dk_h = static_cast<float *>(workspace);
+    float *dk_h = reinterpret_cast<float *>(static_cast<char *>(workspace) + pass_bytes(a, 3, d_k, d_v));
     float *dv_h = dk_h + round256((size_t)a.B * a.T * a.H * d_k * 4) / 4;
-    LinearPass pq = {d_o, v, k, dq, S0, nullptr, a.H, H_kv, H_kv, d_v, d_k};
-    pq.s_in_t = 1;
-    pq.sp = pq.se = scale;
-    pq.sw = 1.f;
-    LinearPass pk = {v, d_o, q, shared ? dk_h : dk, dS_T, nullptr, H_kv, a.H, a.H, d_v, d_k};
-    pk.reverse = pk.s_in_t = 1;
-    pk.out_f32 = shared;
-    pk.sp = pk.sw = scale;
-    pk.se = 1.f;
-    LinearPass pv = {k, q, d_o, shared ? dv_h : dv, dS_T, dS0, H_kv, a.H, a.H, d_k, d_v};
-    pv.reverse = 1;
-    pv.out_f32 = shared;
-    pv.sp = pv.sw = scale;
-    pv.se = 1.f;
-    const LinearPass *passes[] = {&pq, &pk, &pv};
-    for (const LinearPass *p : passes) {
-        const cudaError_t e = run_pass(a, *p, stream, launches);
-        if (e != cudaSuccess) return e;
+    LinearPass p[3] = {{d_o, v, k, dq, S0, nullptr, a.H, H_kv, H_kv, d_v, d_k},
+                       {v, d_o, q, shared ? dk_h : dk, dS_T, nullptr, H_kv, a.H, a.H, d_v, d_k},
+                       {k, q, d_o, shared ? dv_h : dv, dS_T, dS0, H_kv, a.H, a.H, d_k, d_v}};
+    p[0].s_in_t = 1;
+    p[0].sp = p[0].se = scale;
+    p[0].sw = 1.f;
+    for (int i = 1; i < 3; ++i) {
+        p[i].reverse = 1;
+        p[i].out_f32 = shared;
+        p[i].sp = p[i].sw = scale;
+        p[i].se = 1.f;
     }
+    p[1].s_in_t = 1;
+    cudaError_t e = run_passes(a, p, 3, workspace, stream, launches);
+    if (e != cudaSuccess) return e;
     if (!shared) return cudaSuccess;
-    const cudaError_t e = launch_sum_heads(dk_h, dk, a, H_kv, d_k, stream, launches);
+    e = launch_sum_heads(dk_h, dk, a, H_kv, d_k, stream, launches);
     return e == cudaSuccess ? launch_sum_heads(dv_h, dv, a, H_kv, d_v, stream, launches) : e;
 }
 

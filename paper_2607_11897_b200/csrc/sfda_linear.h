@@ -38,6 +38,11 @@ struct LinearArgs {
 // fp32 passes on the warp-level tensor cores (operands split into two tf32 parts).
 cudaError_t launch_linear_f32(const LinearArgs &a, const LinearPass &p, cudaStream_t stream, int *launches);
 
+// bf16 passes on tcgen05.  The workspace begins with the status word that sfda_workspace_status reads.
+size_t linear_tc_bytes(const LinearArgs &a, int passes, int d_k, int d_v);
+cudaError_t launch_linear_tc(const LinearArgs &a, const LinearPass *passes, int count, void *workspace, cudaStream_t stream,
+                             int *launches);
+
 // The entry points' work: passes, and the sums of shared heads' gradients.
 size_t linear_forward_bytes(const LinearArgs &a, int d_k, int d_v);
 cudaError_t launch_linear_forward(const LinearArgs &a, const void *q, const void *k, const void *v, const float *S0, void *o,

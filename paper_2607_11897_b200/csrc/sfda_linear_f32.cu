@@ -258,7 +258,7 @@ cudaError_t dispatch(const LinearArgs &a, const LinearPass &p, cudaStream_t stre
 
 cudaError_t launch_linear_f32(const LinearArgs &a, const LinearPass &p, cudaStream_t stream, int *launches)
 {
-    const cudaError_t e = a.dtype == 1 ? dispatch<__nv_bfloat16>(a, p, stream) : dispatch<float>(a, p, stream);
+    const cudaError_t e = dispatch<float>(a, p, stream);
     if (e == cudaSuccess && launches) ++*launches;
     return e;
 }
