@@ -14,9 +14,9 @@
 // them, which over thousands of tokens would be a bias.  U does not depend on the state, so the serial chain from chunk to
 // chunk is only S <- g S + U, its bf16 copy and O1.
 //
-// Bound by memory (a, b, c read once, out written once).  Twenty warps: TMA, MMA, two idle, four for P and the output, eight for the
-// state, four for w o b.  Two stages of (a, b, c); the high part of w o b replaces b, the low part a, once the products that
-// read them are done.
+// Bound by memory (a, b, c read once, out written once).  28 warps: TMA, MMA, output copies, one idle, eight each for P and the output, for the
+// state and for w o b.  Two stages of (a, b, c); the high part of w o b replaces b and the low part that, once the products that
+// read them are done, and the output leaves through the place of a.
 #include <cuda.h>
 
 #include "sfda_common.cuh"
@@ -29,13 +29,16 @@ namespace {
 using namespace tc;
 
 constexpr int C = 128;                       // tokens per chunk
-constexpr int kThreads = 640;
+constexpr int kThreads = 896;
 constexpr int kNever = 0x7fffffff;
-constexpr int kPairs = 4;                    // sets of `first` in use at a time (see there)
-// warps: 0 TMA, 1 MMA, 4..7 P, 8..15 state, 16..19 keys
-constexpr int kWarpP = 4, kWarpS = 8, kWarpK = 16;
+constexpr int kSets = 4;                     // sets of `first` in use at a time (see there)
+// warps: 0 TMA, 1 MMA, 2 output copies, 4..11 P, 12..19 state, 20..27 keys; registers of a thread of each group (the launch gives 72 to every
+// thread, 504 to seven threads of different groups of four warps, which is what these come to)
+constexpr int kWarpP = 4, kWarpS = 12, kWarpK = 20;
+constexpr int kRegsLaunch = 72, kRegsCtrl = 40, kRegsP = 72, kRegsS = 96, kRegsK = 64;
+static_assert(kRegsCtrl + 2 * (kRegsP + kRegsS + kRegsK) <= 7 * kRegsLaunch, "setmaxnreg draws on the launch's registers");
 
-enum { B_FULL = 0, B_EMPTY = 2, B_A = 4, B_QS, B_KHI, B_KLO, B_P, B_O, B_OFREE, B_S, B_U, kBars };
+enum { B_FULL = 0, B_EMPTY = 2, B_EMPTYA = 4, B_A = 6, B_KHI, B_KV, B_KLO, B_P, B_O, B_OFREE, B_OUT, B_S, B_U, kBars };
 
 struct Pass {
     void *out;
@@ -48,7 +51,7 @@ struct Pass {
 };
 
 struct alignas(64) Params {
-    CUtensorMap map[4];
+    CUtensorMap map[4], out[3];  // inputs; outputs of the passes
     Pass pass[3];
     const float *log_decay;
     const int *lens;
@@ -59,17 +62,18 @@ struct alignas(64) Params {
 // Shared memory: two stages of a, b, c and the bf16 state, then the small things.
 template <int DA, int DC>
 struct Layout {
-    static constexpr int kA = C * DA * 2, kC = C * DC * 2, kStage = 2 * kA + kC;
+    static constexpr int kA = C * DA * 2, kC = C * DC * 2;
+    static constexpr int kB = kA > kC ? kA : kC;       // where b begins: the place of a also takes the output
+    static constexpr int kCat = kB + kA, kStage = kCat + kC;
     static constexpr int kS = 2 * kStage, kMisc = kS + DA * DC * 2;
 };
 struct Misc {
     unsigned long long bars[kBars];
     uint32_t tmem;
     volatile int abort;
-    int any[kPairs];
-    alignas(16) float col[32];
-    float pw[C + 1];
-    int first[kPairs][128];      // by value column: the first token (in the pass's order) whose value was not finite.  Four
+    int any[kSets];
+    float pw[31 + C];            // sp g^m by the distance m from key to query, zeros for the 31 distances of the wrong sign
+    int first[kSets][128];      // by value column: the first token (in the pass's order) whose value was not finite.  Four
                                  // sets, by unit: the keys' warps are at most two units ahead of the last reader
 };
 template <int DA, int DC>
@@ -105,15 +109,51 @@ __device__ __forceinline__ bool elect_one()
     asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(pred));
     return pred != 0;
 }
+template <int N>
+__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// two fp32 values in one instruction
+__device__ __forceinline__ uint64_t two(float x, float y)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void apart(uint64_t v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack2(uint64_t v)
+{
+    float x, y;
+    apart(v, x, y);
+    return pack_bf16(x, y);
+}
+__device__ __forceinline__ uint64_t unpack2(uint32_t w) { return two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 __device__ __forceinline__ void group_sync(int id, int threads) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-// MN-major, 128-byte-swizzled operand: 8 rows of K by 64 elements to an atom of 1024 bytes, `ld` bytes from one block of 64 to
-// the next.
-__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr, uint32_t ld)
-{
-    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(ld >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+// Operand descriptors as two 32-bit halves, of which only the lower one moves along K: the issuing thread spends one addition of
+// a constant on an instruction.  K-major (rows of 128 swizzled bytes): 32 bytes per 16 elements of K.  MN-major (atoms of 8
+// rows of K by 64 elements, `ld` bytes from one block of 64 to the next): 2048 bytes per 16.
+constexpr uint32_t kDescHi = (1024u >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_k(uint32_t saddr) { return saddr >> 4 | 1u << 16; }
+__device__ __forceinline__ uint32_t desc_mn(uint32_t saddr, uint32_t ld) { return saddr >> 4 | (ld >> 4) << 16; }
+constexpr uint32_t kStepMn = 2048 >> 4;
+__device__ __forceinline__ constexpr uint32_t step_k(int k) { return (uint32_t)((k >> 2) * (C * 128 >> 4) + (k & 3) * 2); }   // tiles of C rows
 constexpr uint32_t kMnA = 1u << 15, kMnB = 1u << 16;
+
+// g^n; the zeroth power of a decay that forgets all is 1 too
+__device__ __forceinline__ float power(float log_decay, int n) { return n == 0 ? 1.f : expf((float)n * log_decay); }
 
 // A unit of work: a stretch of the chunks of one pair in one pass.  The two reverse passes of a pair run side by side, for they
 // read the same q and d_o.
@@ -159,18 +199,21 @@ __device__ __forceinline__ void run_tma(unsigned char *smem, Misc &mi, const Par
         for (int i = 0; i < un.hi - un.lo; ++i, ++g) {
             const int st = g & 1, t0 = un.chunk(p, i) * C;
             unsigned char *at = smem + st * Lo::kStage;
+            unsigned long long *bar = &mi.bars[B_FULL + st];
             if (g >= 2 && !wait_warp(mi, B_EMPTY + st, (g >> 1) - 1)) return;
             if (elect_one()) {
-                unsigned long long *bar = &mi.bars[B_FULL + st];
                 mbar_expect_tx(bar, (kStates ? Lo::kA : 2 * Lo::kA) + Lo::kC);
 #pragma unroll
-                for (int x = 0; x < DA / 64; ++x) tma_load_4d(at + Lo::kA + x * C * 128, &p.map[ps.mb], bar, 64 * x, un.h / ps.sb, t0, un.b);
-                if (!kStates)
+                for (int x = 0; x < DA / 64; ++x) tma_load_4d(at + Lo::kB + x * C * 128, &p.map[ps.mb], bar, 64 * x, un.h / ps.sb, t0, un.b);
 #pragma unroll
-                    for (int x = 0; x < DA / 64; ++x) tma_load_4d(at + x * C * 128, &p.map[ps.ma], bar, 64 * x, un.h / ps.sa, t0, un.b);
-#pragma unroll
-                for (int x = 0; x < DC / 64; ++x) tma_load_4d(at + 2 * Lo::kA + x * C * 128, &p.map[ps.mc], bar, 64 * x, un.h / ps.sc, t0, un.b);
+                for (int x = 0; x < DC / 64; ++x) tma_load_4d(at + Lo::kCat + x * C * 128, &p.map[ps.mc], bar, 64 * x, un.h / ps.sc, t0, un.b);
             }
+            __syncwarp();
+            if (kStates) continue;
+            if (g >= 2 && !wait_warp(mi, B_EMPTYA + st, (g >> 1) - 1)) return;     // the output staged there is on its way
+            if (elect_one())
+#pragma unroll
+                for (int x = 0; x < DA / 64; ++x) tma_load_4d(at + x * C * 128, &p.map[ps.ma], bar, 64 * x, un.h / ps.sa, t0, un.b);
             __syncwarp();
         }
     }
@@ -185,19 +228,20 @@ __device__ __forceinline__ void run_mma(unsigned char *smem, Misc &mi, const Par
     constexpr uint32_t kIdA = idesc(C, 0), kIdQS = idesc(DC, 0) | kMnB, kIdKV = idesc(DC, 0) | kMnA | kMnB;
     // DA = 64: the second 64 rows of U repeat the first
     constexpr uint32_t kLdK = DA == 128 ? C * 128 : 0, kLdC = C * 128, kLdS = DA * 128;
+    const uint32_t ss = desc_mn(base + Lo::kS, kLdS);
     int g = 0;
     for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
         const Unit un(p, u, kStates);
         for (int i = 0; i < un.hi - un.lo; ++i, ++g) {
             const int st = g & 1;
-            const uint32_t sa = base + st * Lo::kStage, sb = sa + Lo::kA, sc = sb + Lo::kA, ss = base + Lo::kS;
+            const uint32_t at = base + st * Lo::kStage;
+            const uint32_t a = desc_k(at), b = desc_k(at + Lo::kB), key = desc_mn(at + Lo::kB, kLdK), c = desc_mn(at + Lo::kCat, kLdC);
             if (!wait_warp(mi, B_FULL + st, g >> 1)) return;
             if (!kStates) {
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < DA / 16; ++k)
-                        mma_ss(tA, smem_desc(sa + (k >> 2) * C * 128 + (k & 3) * 32), smem_desc(sb + (k >> 2) * C * 128 + (k & 3) * 32), kIdA, k > 0);
+                    for (int k = 0; k < DA / 16; ++k) mma_ss2(tA, a + step_k(k), kDescHi, b + step_k(k), kDescHi, kIdA, k > 0);
                     mma_commit(&mi.bars[B_A]);
                 }
                 __syncwarp();
@@ -208,24 +252,24 @@ __device__ __forceinline__ void run_mma(unsigned char *smem, Misc &mi, const Par
             if (!kStates) {
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < DA / 16; ++k)
-                        mma_ss(tO1, smem_desc(sa + (k >> 2) * C * 128 + (k & 3) * 32), desc_mn(ss + k * 2048, kLdS), kIdQS, k > 0);
-                    mma_commit(&mi.bars[B_QS]);
+                    for (int k = 0; k < DA / 16; ++k) mma_ss2(tO1, a + step_k(k), kDescHi, ss + k * kStepMn, kDescHi, kIdQS, k > 0);
                 }
                 __syncwarp();
             }
             if (!wait_warp(mi, B_KHI, g)) return;
             tc_fence_after();
-            if (elect_one())
+            if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < C / 16; ++k) mma_ss(tU, desc_mn(sb + k * 2048, kLdK), desc_mn(sc + k * 2048, kLdC), kIdKV, k > 0);
+                for (int k = 0; k < C / 16; ++k) mma_ss2(tU, key + k * kStepMn, kDescHi, c + k * kStepMn, kDescHi, kIdKV, k > 0);
+                mma_commit(&mi.bars[B_KV]);
+            }
             __syncwarp();
             if (!kStates) {
                 if (!wait_warp(mi, B_P, g)) return;
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < C / 16; ++k) mma_ts(tO2, tA + 8 * k, desc_mn(sc + k * 2048, kLdC), kIdQS, k > 0);
+                    for (int k = 0; k < C / 16; ++k) mma_ts2(tO2, tA + (k >> 2) * 64 + (k & 3) * 8, c + k * kStepMn, kDescHi, kIdQS, k > 0);
                     mma_commit(&mi.bars[B_O]);
                 }
                 __syncwarp();
@@ -234,7 +278,7 @@ __device__ __forceinline__ void run_mma(unsigned char *smem, Misc &mi, const Par
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < C / 16; ++k) mma_ss(tU, desc_mn(sa + k * 2048, kLdK), desc_mn(sc + k * 2048, kLdC), kIdKV, 1);
+                for (int k = 0; k < C / 16; ++k) mma_ss2(tU, key + k * kStepMn, kDescHi, c + k * kStepMn, kDescHi, kIdKV, 1);
                 mma_commit(&mi.bars[B_U]);
                 mma_commit(&mi.bars[B_EMPTY + st]);
             }
@@ -243,12 +287,20 @@ __device__ __forceinline__ void run_mma(unsigned char *smem, Misc &mi, const Par
     }
 }
 
-// P and the output: thread t has row t of the chunk
+// Outputs leave through the place of a and a tensor copy (32 rows of a warp's own stores lie in 32 different lines, which cost
+// 4000 of 7300 cycles of a chunk); not those in fp32, which have no room there, nor a sequence's last rows where other rows follow
+// that have to stay as they are.
+__device__ __forceinline__ bool store_directly(const Params &p, const Pass &ps, int t0, int n) { return ps.out_f32 || (n < C && t0 + n < p.T); }
+
+// P and the output: a thread has row t of the chunk and one half of the columns
 template <int DA, int DC>
-__device__ __forceinline__ void run_p(Misc &mi, const Params &p, uint32_t tmem)
+__device__ __forceinline__ void run_p(unsigned char *smem, Misc &mi, const Params &p, uint32_t tmem)
 {
-    const int t = threadIdx.x - kWarpP * 32, w = t >> 5;
-    const uint32_t lane = tmem + ((uint32_t)(w * 32) << 16), tA = lane, tO1 = lane + 256, tO2 = lane + 384;
+    const int id = threadIdx.x - kWarpP * 32, t = id & 127, w = t >> 5, half = id >> 7;
+    const uint32_t lane = tmem + ((uint32_t)(w * 32) << 16);
+    // the half's P goes over the half's own part of A, which its threads have read by then
+    const uint32_t base = smem_u32(smem);
+    const uint32_t tA = lane + 64 * half, tO1 = lane + 256 + (DC / 2) * half, tO2 = tO1 + 128;
     bool live = true;                          // after a wait that ran out a warp only keeps the group's barriers company
     int g = 0, nth = 0;                        // chunks and units with chunks so far
     for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
@@ -257,88 +309,116 @@ __device__ __forceinline__ void run_p(Misc &mi, const Params &p, uint32_t tmem)
         const bool rev = ps.reverse != 0;
         const float ld = p.log_decay[un.h];
         if (un.hi == un.lo) continue;
-        const int set = nth++ & (kPairs - 1);
-        group_sync(1, 128);                    // the tables' readers are done with the last unit's
-        mi.pw[t] = t == 0 ? 1.f : expf((float)t * ld);
-        if (t == 0) mi.pw[C] = expf((float)C * ld);
-        group_sync(1, 128);
-        if (t < 32) mi.col[t] = rev ? mi.pw[t] : mi.pw[31 - t];
-        group_sync(1, 128);
+        const int set = nth++ & (kSets - 1);
+        group_sync(1, 256);                    // the tables' readers are done with the last unit's
+        // forward: pw[31 + m], m = t - i from -31 to 127; reverse: pw[127 + m], m from -127 to 31
+        if (id < 31 + C) mi.pw[id] = (rev ? id > C - 1 : id < 31) ? 0.f : ps.sp * power(ld, rev ? C - 1 - id : id - 31);
+        const float *pw = mi.pw + (rev ? C - 1 : 31);
+        const float e_full = ps.se * power(ld, rev ? C - 1 - t : t + 1);
+        group_sync(1, 256);
         for (int i = 0; i < un.hi - un.lo; ++i, ++g) {
             const int t0 = un.chunk(p, i) * C, n = min(C, un.len - t0);
             if (!(live = live && wait_warp(mi, B_A, g))) continue;
             tc_fence_after();
+            // One loop for blocks on and off the diagonal, with the power of each entry from the table: the kernel's code is
+            // read from the instruction cache by warps of four roles at once, and less of it was worth more than fewer loads.
 #pragma unroll 1
-            for (int j = 0; j < 4; ++j) {
+            for (int x = 0; x < 2; ++x) {
+                const int j = 2 * half + x, m = t - 32 * j;        // the block of 32 tokens; the distance to its first
                 uint32_t y[16];
-                if (rev ? j < w : j > w) {
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) y[x] = 0;
-                } else {
+                for (int z = 0; z < 16; ++z) y[z] = 0;
+                if (rev ? j >= w : j <= w) {
                     float v[32];
-                    tmem_ld<32>(tA + 32 * j, reinterpret_cast<uint32_t *>(v));
+                    tmem_ld<32>(tA + 32 * x, reinterpret_cast<uint32_t *>(v));
+                    const float *d = pw + m;
+                    // tokens of the block that the row reads: z <= m, or m <= z < n - 32 j
+                    const int lo = rev ? max(m, 0) : 0, hi = rev ? min(n - 32 * j, 32) : min(m + 1, 32);
+                    const uint32_t keep = (hi <= lo ? 0u : 0xffffffffu >> (32 - hi)) & (lo > 31 ? 0u : 0xffffffffu << lo);
                     tc_wait_ld();
-                    if (j != w) {
-                        const float row = ps.sp * mi.pw[rev ? 32 * j - t : t - (32 * j + 31)];
 #pragma unroll
-                        for (int x = 0; x < 32; x += 4) {
-                            const float4 c = *reinterpret_cast<const float4 *>(&mi.col[x]);
-                            v[x] *= row * c.x; v[x + 1] *= row * c.y; v[x + 2] *= row * c.z; v[x + 3] *= row * c.w;
-                        }
-                    } else {
-                        const int tt = t & 31;
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) {
-                            const int gap = rev ? x - tt : tt - x;
-                            v[x] = gap >= 0 ? v[x] * (ps.sp * mi.pw[gap & 31]) : 0.f;
-                        }
+                    for (int z = 0; z < 32; z += 2) {
+                        const float f0 = d[-z], f1 = d[-z - 1];
+                        const float q0 = v[z] * f0, q1 = v[z + 1] * f1;
+                        y[z / 2] = pack_bf16(keep & (1u << z) ? q0 : 0.f, keep & (2u << z) ? q1 : 0.f);
                     }
-                    if (rev && 32 * j + 32 > n)
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) v[x] = 32 * j + x < n ? v[x] : 0.f;
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) y[x] = pack_bf16(v[2 * x], v[2 * x + 1]);
                 }
-                tmem_st16(tA + 16 * j, y);     // the columns under it are read already
+                tmem_st16(tA + 16 * x, y);
             }
             tc_wait_st();
             tc_fence_before();
             arrive(mi, B_P);
-            if (!(live = wait_warp(mi, B_O, g))) continue;
+            const float e = rev && n < C ? ps.se * power(ld, max(n - 1 - t, 0)) : e_full;
+            const uint64_t ee = two(e, e);
+            if (!(live = wait_warp(mi, B_O, g))) continue;     // (a S is done by then, and with it the last reading of a)
             tc_fence_after();
-            const float e = ps.se * mi.pw[rev ? max(n - 1 - t, 0) : t + 1];
-            const bool bad = mi.any[set] != 0;
+            const bool bad = mi.any[set] != 0, direct = store_directly(p, ps, t0, n);
             const int order = rev ? un.len - 1 - (t0 + t) : t0 + t;
-            const size_t row = (((size_t)un.b * p.T + t0 + t) * p.H + un.h) * DC;
+            const uint32_t stage = base + (g & 1) * Layout<DA, DC>::kStage;
 #pragma unroll 1
-            for (int j = 0; j < DC / 32; ++j) {
-                float v[32], s[32];
-                tmem_ld<32>(tO1 + 32 * j, reinterpret_cast<uint32_t *>(s));
-                tmem_ld<32>(tO2 + 32 * j, reinterpret_cast<uint32_t *>(v));
+            for (int j = 0; j < DC / 2; j += 16) {
+                const int col = (DC / 2) * half + j;
+                float v[16], s[16];
+                tmem_ld<16>(tO1 + j, reinterpret_cast<uint32_t *>(s));
+                tmem_ld<16>(tO2 + j, reinterpret_cast<uint32_t *>(v));
                 tc_wait_ld();
-                if (j == DC / 32 - 1) {
-                    tc_fence_before();
-                    arrive(mi, B_OFREE);
+#pragma unroll
+                for (int x = 0; x < 16; x += 2) apart(fma2(ee, two(s[x], s[x + 1]), two(v[x], v[x + 1])), v[x], v[x + 1]);
+                if (bad) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x)
+                        if (order >= mi.first[set][col + x]) v[x] = __int_as_float(0x7fffffff);
                 }
+                if (direct && ps.out_f32) {
+                    float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(ps.out) + (((size_t)un.b * p.T + t0 + t) * p.H + un.h) * DC + col);
+                    if (t < n)
 #pragma unroll
-                for (int x = 0; x < 32; ++x) v[x] = fmaf(e, s[x], v[x]);
-                if (bad)
+                        for (int x = 0; x < 4; ++x) o[x] = make_float4(v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]);
+                    continue;
+                }
+                uint32_t y[8];
 #pragma unroll
-                    for (int x = 0; x < 32; ++x)
-                        if (order >= mi.first[set][32 * j + x]) v[x] = __int_as_float(0x7fffffff);
-                if (t >= n) continue;
-                if (ps.out_f32) {
-                    float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(ps.out) + row + 32 * j);
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) o[x] = make_float4(v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]);
-                } else {
-                    uint4 *o = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(ps.out) + row + 32 * j);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        o[x] = make_uint4(pack_bf16(v[8 * x], v[8 * x + 1]), pack_bf16(v[8 * x + 2], v[8 * x + 3]),
-                                          pack_bf16(v[8 * x + 4], v[8 * x + 5]), pack_bf16(v[8 * x + 6], v[8 * x + 7]));
+                for (int x = 0; x < 8; ++x) y[x] = pack_bf16(v[2 * x], v[2 * x + 1]);
+                if (!direct) {
+                    const uint32_t at = stage + (col >> 6) * C * 128;
+                    sts128(at + sw_off(t, col & 63), y[0], y[1], y[2], y[3]);
+                    sts128(at + sw_off(t, (col & 63) + 8), y[4], y[5], y[6], y[7]);
+                } else if (t < n) {
+                    uint4 *o = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(ps.out) + (((size_t)un.b * p.T + t0 + t) * p.H + un.h) * DC + col);
+                    o[0] = make_uint4(y[0], y[1], y[2], y[3]);
+                    o[1] = make_uint4(y[4], y[5], y[6], y[7]);
                 }
             }
+            tc_fence_before();
+            arrive(mi, B_OFREE);
+            if (!direct) fence_async_smem();
+            arrive(mi, B_OUT);
+        }
+    }
+}
+
+// The staged outputs' copies to memory (one warp; rows behind T are cut off by the tensor map)
+template <int DA, int DC>
+__device__ __forceinline__ void run_out(unsigned char *smem, Misc &mi, const Params &p)
+{
+    int g = 0;
+    for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
+        const Unit un(p, u, false);
+        const Pass &ps = p.pass[un.pass];
+        for (int i = 0; i < un.hi - un.lo; ++i, ++g) {
+            const int t0 = un.chunk(p, i) * C, n = min(C, un.len - t0);
+            if (!wait_warp(mi, B_OUT, g)) return;
+            if (elect_one()) {
+                if (!store_directly(p, ps, t0, n)) {
+#pragma unroll
+                    for (int x = 0; x < DC / 64; ++x)
+                        tma_store_4d(&p.out[un.pass], smem + (g & 1) * Layout<DA, DC>::kStage + x * C * 128, 64 * x, un.h, t0, un.b);
+                    tma_store_commit();
+                    tma_store_wait_read();
+                }
+                arrive(mi, B_EMPTYA + (g & 1));
+            }
+            __syncwarp();
         }
     }
 }
@@ -358,20 +438,22 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
         const Unit un(p, u, kStates);
         const Pass &ps = p.pass[un.pass];
         const float ld = p.log_decay[un.h];
-        float s[N];
+        uint64_t s[N / 2];                     // two columns each
 #pragma unroll
-        for (int x = 0; x < N; ++x) s[x] = 0.f;
+        for (int x = 0; x < N / 2; ++x) s[x] = 0;
         if (!kStates && mine) {
             if (ps.s_in) {
                 const size_t at = (size_t)un.pair * DA * DC;
                 if (ps.s_in_t) {
 #pragma unroll
-                    for (int x = 0; x < N; ++x) s[x] = ps.s_in[at + (size_t)(c0 + x) * DA + k];
+                    for (int x = 0; x < N; x += 2)
+                        s[x / 2] = two(ps.s_in[at + (size_t)(c0 + x) * DA + k], ps.s_in[at + (size_t)(c0 + x + 1) * DA + k]);
                 } else {
 #pragma unroll
                     for (int x = 0; x < N; x += 4) {
                         const float4 v = *reinterpret_cast<const float4 *>(ps.s_in + at + (size_t)k * DC + c0 + x);
-                        s[x] = v.x; s[x + 1] = v.y; s[x + 2] = v.z; s[x + 3] = v.w;
+                        s[x / 2] = two(v.x, v.y);
+                        s[x / 2 + 1] = two(v.z, v.w);
                     }
                 }
             }
@@ -380,12 +462,13 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
                 const int tok = un.tokens(p, j);
                 if (tok == 0) continue;
                 const float gn = expf((float)tok * ld);
+                const uint64_t gg = two(gn, gn);
                 const float *from = ps.seg + ((size_t)un.pair * (p.nseg - 1) + j) * DA * DC + (size_t)k * DC + c0;
 #pragma unroll
                 for (int x = 0; x < N; x += 4) {
                     const float4 v = __ldcg(reinterpret_cast<const float4 *>(from + x));
-                    s[x] = fmaf(gn, s[x], v.x); s[x + 1] = fmaf(gn, s[x + 1], v.y);
-                    s[x + 2] = fmaf(gn, s[x + 2], v.z); s[x + 3] = fmaf(gn, s[x + 3], v.w);
+                    s[x / 2] = fma2(gg, s[x / 2], two(v.x, v.y));
+                    s[x / 2 + 1] = fma2(gg, s[x / 2 + 1], two(v.z, v.w));
                 }
             }
         }
@@ -398,16 +481,20 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
                 const float x0 = (float)n * ld;
                 const bool weak = x0 > -0.5f;
                 const float gm = weak ? expm1f(x0) : expf(x0);
+                const uint64_t gg = two(gm, gm), one = weak ? two(1.f, 1.f) : 0;
                 if (!wait_warp(mi, B_U, g)) return;
                 tc_fence_after();
                 ++g;
 #pragma unroll
                 for (int x = 0; x < N; x += 16) {
-                    float v[16];
-                    tmem_ld<16>(tU + x, reinterpret_cast<uint32_t *>(v));
+                    uint32_t v[16];
+                    tmem_ld<16>(tU + x, v);
                     tc_wait_ld();
 #pragma unroll
-                    for (int y = 0; y < 16; ++y) s[x + y] = weak ? fmaf(gm, s[x + y], s[x + y]) + v[y] : fmaf(gm, s[x + y], v[y]);
+                    for (int y = 0; y < 16; y += 2) {
+                        uint64_t &z = s[(x + y) / 2];
+                        z = fma2(gg, z, fma2(one, z, two(__uint_as_float(v[y]), __uint_as_float(v[y + 1]))));
+                    }
                 }
                 tc_fence_before();
             }
@@ -416,8 +503,8 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
 #pragma unroll
                 for (int x = 0; x < N; x += 8) {
                     const int col = c0 + x;
-                    sts128(ss + (col >> 6) * (DA * 128) + sw_off(k, col & 63), pack_bf16(s[x], s[x + 1]), pack_bf16(s[x + 2], s[x + 3]),
-                           pack_bf16(s[x + 4], s[x + 5]), pack_bf16(s[x + 6], s[x + 7]));
+                    sts128(ss + (col >> 6) * (DA * 128) + sw_off(k, col & 63), pack2(s[x / 2]), pack2(s[x / 2 + 1]), pack2(s[x / 2 + 2]),
+                           pack2(s[x / 2 + 3]));
                 }
             }
             if (!kStates) fence_async_smem();
@@ -426,25 +513,34 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
         float *to = kStates ? ps.seg + ((size_t)un.pair * (p.nseg - 1) + un.seg) * DA * DC
                             : un.seg == p.nseg - 1 && ps.s_out ? ps.s_out + (size_t)un.pair * DA * DC : nullptr;
         if (to && mine) {
-            const int set = (nth - 1) & (kPairs - 1);
-            if (chunks > 0 && mi.any[set])
+            const int set = (nth - 1) & (kSets - 1);
+            const bool bad = chunks > 0 && mi.any[set];
 #pragma unroll
-                for (int x = 0; x < N; ++x)
-                    if (mi.first[set][c0 + x] != kNever) s[x] = __int_as_float(0x7fffffff);
-#pragma unroll
-            for (int x = 0; x < N; x += 4)
-                *reinterpret_cast<float4 *>(to + (size_t)k * DC + c0 + x) = make_float4(s[x], s[x + 1], s[x + 2], s[x + 3]);
+            for (int x = 0; x < N; x += 4) {
+                float4 v;
+                apart(s[x / 2], v.x, v.y);
+                apart(s[x / 2 + 1], v.z, v.w);
+                if (bad) {
+                    const float nan = __int_as_float(0x7fffffff);
+                    const int *f = &mi.first[set][c0 + x];
+                    v = make_float4(f[0] != kNever ? nan : v.x, f[1] != kNever ? nan : v.y, f[2] != kNever ? nan : v.z, f[3] != kNever ? nan : v.w);
+                }
+                *reinterpret_cast<float4 *>(to + (size_t)k * DC + c0 + x) = v;
+            }
         }
     }
 }
 
-// w o b in two parts, and c made safe: thread r has token r of the chunk
+// w o b in two parts, and c made safe: a thread has token r of the chunk and one half of the channels
 template <int DA, int DC, bool kStates>
 __device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Params &p)
 {
     using Lo = Layout<DA, DC>;
-    const int r = threadIdx.x - kWarpK * 32;
+    constexpr int NA = DA / 2, NC = DC / 2;
+    const int id = threadIdx.x - kWarpK * 32, r = id & 127, half = id >> 7;
     const uint32_t base = smem_u32(smem);
+    // byte offset of channel `ch` (a multiple of 8) of the thread's token in a tile
+    const auto off = [r](int ch) { return (ch >> 6) * C * 128 + sw_off(r, ch & 63); };
     bool live = true;                          // as in run_p
     int g = 0, nth = 0;                        // chunks and units with chunks so far
     for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
@@ -454,28 +550,30 @@ __device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Pa
         const float ld = p.log_decay[un.h];
         const int chunks = un.hi - un.lo;
         if (chunks == 0) continue;
-        const int set = nth++ & (kPairs - 1);
-        mi.first[set][r] = kNever;
-        if (r == 0) mi.any[set] = 0;
-        group_sync(2, 128);
+        const int set = nth++ & (kSets - 1);
+        if (half == 0) mi.first[set][r] = kNever;
+        if (id == 0) mi.any[set] = 0;
+        group_sync(2, 256);
         for (int i = 0; i < chunks; ++i, ++g) {
             const int st = g & 1, t0 = un.chunk(p, i) * C, n = min(C, un.len - t0);
-            const uint32_t sa = base + st * Lo::kStage, sb = sa + Lo::kA, sc = sb + Lo::kA;
+            const uint32_t sb = base + st * Lo::kStage + Lo::kB, sc = base + st * Lo::kStage + Lo::kCat;
+            const int hops = rev ? r + 1 : n - 1 - r;
+            const float w = ps.sw * power(ld, max(hops, 0));
             if (!(live = live && wait_warp(mi, B_FULL + st, g >> 1))) continue;
             uint32_t odd = 0;
 #pragma unroll
-            for (int x = 0; x < DC; x += 8) {
-                const uint4 v = lds128(sc + (x >> 6) * C * 128 + sw_off(r, x & 63));
+            for (int x = 0; x < NC; x += 8) {
+                const uint4 v = lds128(sc + off(half * NC + x));
                 odd |= ((v.x & 0x7fff7fffu) + 0x00800080u) | ((v.y & 0x7fff7fffu) + 0x00800080u) | ((v.z & 0x7fff7fffu) + 0x00800080u) |
                        ((v.w & 0x7fff7fffu) + 0x00800080u);
             }
             if (r >= n) {                      // behind the end: whatever is there is no value
 #pragma unroll 1
-                for (int x = 0; x < DC; x += 8) sts128(sc + (x >> 6) * C * 128 + sw_off(r, x & 63), 0, 0, 0, 0);
+                for (int x = 0; x < NC; x += 8) sts128(sc + off(half * NC + x), 0, 0, 0, 0);
             } else if (odd & 0x80008000u) {
 #pragma unroll 1
-                for (int x = 0; x < DC; ++x) {
-                    const uint32_t at = sc + (x >> 6) * C * 128 + sw_off(r, x & 63);
+                for (int x = half * NC; x < (half + 1) * NC; ++x) {
+                    const uint32_t at = sc + off(x);
                     if ((lds16(at) & 0x7f80u) == 0x7f80u) {
                         sts16(at, 0);
                         atomicMin(&mi.first[set][x], rev ? un.len - 1 - (t0 + r) : t0 + r);
@@ -483,30 +581,35 @@ __device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Pa
                     }
                 }
             }
-            const int hops = rev ? r + 1 : n - 1 - r;
-            const float w = r < n ? ps.sw * (hops == 0 ? 1.f : expf((float)hops * ld)) : 0.f;
             if (!kStates && !(live = wait_warp(mi, B_A, g))) continue;
-            uint32_t lo[DA / 2];
+            uint32_t lo[NA / 2];
+            if (r < n) {
+                const uint64_t ww = two(w, w), minus = two(-1.f, -1.f);
 #pragma unroll
-            for (int x = 0; x < DA; x += 8) {
-                const uint32_t at = sb + (x >> 6) * C * 128 + sw_off(r, x & 63);
-                const uint4 v = lds128(at);
-                const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-                uint32_t hi[4];
+                for (int x = 0; x < NA; x += 8) {
+                    const uint32_t at = sb + off(half * NA + x);
+                    const uint4 v = lds128(at);
+                    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                    uint32_t hi[4];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const float f0 = r < n ? w * __uint_as_float(in[y] << 16) : 0.f, f1 = r < n ? w * __uint_as_float(in[y] & 0xffff0000u) : 0.f;
-                    hi[y] = pack_bf16(f0, f1);
-                    lo[x / 2 + y] = pack_bf16(f0 - __uint_as_float(hi[y] << 16), f1 - __uint_as_float(hi[y] & 0xffff0000u));
+                    for (int y = 0; y < 4; ++y) {
+                        const uint64_t f = mul2(unpack2(in[y]), ww);
+                        hi[y] = pack2(f);
+                        lo[x / 2 + y] = pack2(fma2(unpack2(hi[y]), minus, f));
+                    }
+                    sts128(at, hi[0], hi[1], hi[2], hi[3]);
                 }
-                sts128(at, hi[0], hi[1], hi[2], hi[3]);
+            } else {
+#pragma unroll
+                for (int x = 0; x < NA / 2; ++x) lo[x] = 0;
+#pragma unroll
+                for (int x = 0; x < NA; x += 8) sts128(sb + off(half * NA + x), 0, 0, 0, 0);
             }
             fence_async_smem();
             arrive(mi, B_KHI);
-            if (!kStates && !(live = wait_warp(mi, B_QS, g))) continue;
+            if (!(live = wait_warp(mi, B_KV, g))) continue;
 #pragma unroll
-            for (int x = 0; x < DA; x += 8)
-                sts128(sa + (x >> 6) * C * 128 + sw_off(r, x & 63), lo[x / 2], lo[x / 2 + 1], lo[x / 2 + 2], lo[x / 2 + 3]);
+            for (int x = 0; x < NA; x += 8) sts128(sb + off(half * NA + x), lo[x / 2], lo[x / 2 + 1], lo[x / 2 + 2], lo[x / 2 + 3]);
             fence_async_smem();
             arrive(mi, B_KLO);
         }
@@ -520,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, 1) sfda_linear_tc_kernel(const __gri
     Misc &mi = *reinterpret_cast<Misc *>(smem + Layout<DA, DC>::kMisc);
     const int tid = threadIdx.x, warp = tid >> 5;
     if (tid == 0) {
-        const int counts[kBars] = {1, 1, 1, 1, 1, 1, 128, 128, 128, 1, 128, 256, 1};
+        const int counts[kBars] = {1, 1, 1, 1, 1, 1, 1, 256, 1, 256, 256, 1, 256, 256, 256, 1};
         for (int i = 0; i < kBars; ++i) mbar_init(&mi.bars[i], counts[i]);
         mi.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -534,11 +637,20 @@ __global__ void __launch_bounds__(kThreads, 1) sfda_linear_tc_kernel(const __gri
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = mi.tmem;
-    if (warp == 0) run_tma<DA, DC, kStates>(smem, mi, p);
-    else if (warp == 1) run_mma<DA, DC, kStates>(smem, mi, p, tmem);
-    else if (warp >= kWarpK) run_keys<DA, DC, kStates>(smem, mi, p);
-    else if (warp >= kWarpS) run_state<DA, DC, kStates>(smem, mi, p, tmem);
-    else if (warp >= kWarpP && !kStates) run_p<DA, DC>(mi, p, tmem);
+    if (warp < kWarpP) {
+        regs_dec<kRegsCtrl>();
+        if (warp == 0) run_tma<DA, DC, kStates>(smem, mi, p);
+        if (warp == 1) run_mma<DA, DC, kStates>(smem, mi, p, tmem);
+        if (warp == 2 && !kStates) run_out<DA, DC>(smem, mi, p);
+    } else if (warp >= kWarpK) {
+        regs_dec<kRegsK>();
+        run_keys<DA, DC, kStates>(smem, mi, p);
+    } else if (warp >= kWarpS) {
+        regs_inc<kRegsS>();
+        run_state<DA, DC, kStates>(smem, mi, p, tmem);
+    } else if (!kStates) {
+        run_p<DA, DC>(smem, mi, p, tmem);
+    }
     tc_fence_before();
     __syncthreads();
     if (mi.abort) {
@@ -701,7 +813,8 @@ cudaError_t launch_linear_tc(const LinearArgs &a, const LinearPass *passes, int 
             y.out = x.out; y.s_in = x.s_in; y.s_out = x.s_out;
             y.seg = seg + i * each * (p.nseg - 1);
             y.ma = map_of(x.a, x.Ha, DA); y.mb = map_of(x.b, x.Hb, DA); y.mc = map_of(x.c, x.Hc, DC);
-            if (y.ma < 0 || y.mb < 0 || y.mc < 0) return cudaErrorInvalidValue;
+            if (y.ma < 0 || y.mb < 0 || y.mc < 0 || (!x.out_f32 && !make_map(&p.out[i], x.out, a.B, a.T, a.H, DC)))
+                return cudaErrorInvalidValue;
             y.sa = a.H / x.Ha; y.sb = a.H / x.Hb; y.sc = a.H / x.Hc;
             y.reverse = x.reverse; y.s_in_t = x.s_in_t; y.out_f32 = x.out_f32;
             y.sp = x.sp; y.se = x.se; y.sw = x.sw;
