@@ -16,7 +16,7 @@
 //
 // Bound by memory (a, b, c read once, out written once).  28 warps: TMA, MMA, output copies, one idle, eight each for P and the output, for the
 // state and for w o b.  Two stages of (a, b, c); the high part of w o b replaces b and the low part that, once the products that
-// read them are done, and the output leaves through the place of a.
+// read them are done, and the output leaves through the place of c.
 #include <cuda.h>
 
 #include "sfda_common.cuh"
@@ -31,14 +31,17 @@ using namespace tc;
 constexpr int C = 128;                       // tokens per chunk
 constexpr int kThreads = 896;
 constexpr int kNever = 0x7fffffff;
-constexpr int kSets = 4;                     // sets of `first` in use at a time (see there)
+constexpr int kSets = 3;                     // sets of `first` in use at a time (see there)
 // warps: 0 TMA, 1 MMA, 2 output copies, 4..11 P, 12..19 state, 20..27 keys; registers of a thread of each group (the launch gives 72 to every
 // thread, 504 to seven threads of different groups of four warps, which is what these come to)
 constexpr int kWarpP = 4, kWarpS = 12, kWarpK = 20;
 constexpr int kRegsLaunch = 72, kRegsCtrl = 40, kRegsP = 72, kRegsS = 96, kRegsK = 64;
 static_assert(kRegsCtrl + 2 * (kRegsP + kRegsS + kRegsK) <= 7 * kRegsLaunch, "setmaxnreg draws on the launch's registers");
 
-enum { B_FULL = 0, B_EMPTY = 2, B_EMPTYA = 4, B_A = 6, B_KHI, B_KV, B_KLO, B_P, B_O, B_OFREE, B_OUT, B_S, B_U, kBars };
+// tensor memory: A (and P over it), U, O, the two parts of w o b
+constexpr uint32_t kColA = 0, kColU = 128, kColO = 256, kColK = 384;
+
+enum { B_FULL = 0, B_FULLC = 2, B_EMPTY = 4, B_EMPTYC = 6, B_A = 8, B_QS, B_K, B_U, B_P, B_O, B_OFREE, B_OUT, B_S, B_E, kBars };
 
 struct Pass {
     void *out;
@@ -63,8 +66,7 @@ struct alignas(64) Params {
 template <int DA, int DC>
 struct Layout {
     static constexpr int kA = C * DA * 2, kC = C * DC * 2;
-    static constexpr int kB = kA > kC ? kA : kC;       // where b begins: the place of a also takes the output
-    static constexpr int kCat = kB + kA, kStage = kCat + kC;
+    static constexpr int kCat = 2 * kA, kStage = kCat + kC;      // a, b, c
     static constexpr int kS = 2 * kStage, kMisc = kS + DA * DC * 2;
 };
 struct Misc {
@@ -72,32 +74,36 @@ struct Misc {
     uint32_t tmem;
     volatile int abort;
     int any[kSets];
-    float pw[31 + C];            // sp g^m by the distance m from key to query, zeros for the 31 distances of the wrong sign
-    int first[kSets][128];      // by value column: the first token (in the pass's order) whose value was not finite.  Four
+    alignas(16) float pw[31 + C];// the powers of g that make P (see run_p)
+    int first[kSets][128];      // by value column: the first token (in the pass's order) whose value was not finite.  Three
                                  // sets, by unit: the keys' warps are at most two units ahead of the last reader
 };
 template <int DA, int DC>
 constexpr int kSmem = Layout<DA, DC>::kMisc + (int)sizeof(Misc);
 
-__device__ __forceinline__ bool wait_k(Misc &mi, int bar, int k)
+// Wait for completion number k of a barrier, with one outcome for the warp.  try_wait parks the warp in hardware for up to 20 us
+// at a time; after kTries of them (seconds), or when another wait of the CTA has given up, it gives up and says so.  A few
+// instructions, for it is inlined at every wait: the loops of all roles have to stay in the SM's instruction cache together.
+constexpr int kTries = 1 << 17;
+__device__ __forceinline__ bool wait_warp(Misc &mi, int bar, int k)
 {
     const uint32_t addr = smem_u32(&mi.bars[bar]), parity = (uint32_t)k & 1u;
-    const uint32_t t0 = (uint32_t)clock();
-    do {
+#pragma unroll 1
+    for (int n = 0; n < kTries; ++n) {
         uint32_t ok;
         asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}\n"
                      : "=r"(ok)
                      : "r"(addr), "r"(parity), "r"(20000u)
                      : "memory");
-        if (ok) {
+        if (__all_sync(0xffffffffu, ok)) {
             chaos(addr + 77u);
             return true;
         }
-    } while (!mi.abort && (uint32_t)clock() - t0 < 0x80000000u);
+        if (__any_sync(0xffffffffu, mi.abort)) break;
+    }
     mi.abort = 1;
     return false;
 }
-__device__ __forceinline__ bool wait_warp(Misc &mi, int bar, int k) { return __all_sync(0xffffffffu, wait_k(mi, bar, k) ? 1 : 0) != 0; }
 __device__ __forceinline__ void arrive(Misc &mi, int bar)
 {
     chaos(bar);
@@ -108,6 +114,22 @@ __device__ __forceinline__ bool elect_one()
     uint32_t pred;
     asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(pred));
     return pred != 0;
+}
+// Four 8 x 8 blocks of 16-bit elements, transposed: lane l gives the address of row l % 8 of block l / 8; register k of thread T
+// holds (column T / 4; rows 2 (T % 4), + 1) of block k.
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t saddr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(saddr)
+                 : "memory");
+}
+// 16 lanes x 16 columns: registers 2 i, 2 i + 1 of thread T are column 4 i + T % 4 of lanes T / 4, T / 4 + 8.
+__device__ __forceinline__ void tmem_st_16x128b_x4(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 template <int N>
 __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -150,7 +172,12 @@ __device__ __forceinline__ uint32_t desc_k(uint32_t saddr) { return saddr >> 4 |
 __device__ __forceinline__ uint32_t desc_mn(uint32_t saddr, uint32_t ld) { return saddr >> 4 | (ld >> 4) << 16; }
 constexpr uint32_t kStepMn = 2048 >> 4;
 __device__ __forceinline__ constexpr uint32_t step_k(int k) { return (uint32_t)((k >> 2) * (C * 128 >> 4) + (k & 3) * 2); }   // tiles of C rows
-constexpr uint32_t kMnA = 1u << 15, kMnB = 1u << 16;
+constexpr uint32_t kMnB = 1u << 16;           // instruction descriptor: B is MN-major
+
+// out_t = e_t (a_t S + sum_i (P_ti / e_t) c_i): with P / e the two products share an accumulator, and P / e needs no power of the
+// row at all, only (sp / se) g^-(i + 1) (reverse: g^(i - n + 1)) of the column.  These stay below 2^40 for g >= 0.805; for heads
+// that forget faster a S is multiplied by e in the accumulator before P c is added.
+__device__ __forceinline__ bool shares(float log_decay, const Pass &ps) { return log_decay >= -0.2166f && ps.se != 0.f; }
 
 // g^n; the zeroth power of a decay that forgets all is 1 too
 __device__ __forceinline__ float power(float log_decay, int n) { return n == 0 ? 1.f : expf((float)n * log_decay); }
@@ -188,34 +215,52 @@ struct Unit {
     }
 };
 
+// The chunks of a CTA one after another
+struct Cursor {
+    int u, i;
+    bool states;
+    Unit un;
+    __device__ __forceinline__ Cursor(const Params &p, bool st) : u(blockIdx.x), i(0), states(st), un(p, min((int)blockIdx.x, p.units - 1), st) { skip(p); }
+    __device__ __forceinline__ void skip(const Params &p)      // units without a chunk
+    {
+        while (u < p.units && i >= un.hi - un.lo) {
+            u += gridDim.x;
+            i = 0;
+            if (u < p.units) un = Unit(p, u, states);
+        }
+    }
+    __device__ __forceinline__ void next(const Params &p) { ++i; skip(p); }
+};
+
 template <int DA, int DC, bool kStates>
 __device__ __forceinline__ void run_tma(unsigned char *smem, Misc &mi, const Params &p)
 {
     using Lo = Layout<DA, DC>;
     int g = 0;
-    for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
-        const Unit un(p, u, kStates);
+    for (Cursor cur(p, kStates); cur.u < p.units; cur.next(p), ++g) {
+        const Unit &un = cur.un;
         const Pass &ps = p.pass[un.pass];
-        for (int i = 0; i < un.hi - un.lo; ++i, ++g) {
-            const int st = g & 1, t0 = un.chunk(p, i) * C;
-            unsigned char *at = smem + st * Lo::kStage;
+        const int st = g & 1, t0 = un.chunk(p, cur.i) * C;
+        unsigned char *at = smem + st * Lo::kStage;
+        if (g >= 2 && !wait_warp(mi, B_EMPTY + st, (g >> 1) - 1)) return;
+        if (elect_one()) {
             unsigned long long *bar = &mi.bars[B_FULL + st];
-            if (g >= 2 && !wait_warp(mi, B_EMPTY + st, (g >> 1) - 1)) return;
-            if (elect_one()) {
-                mbar_expect_tx(bar, (kStates ? Lo::kA : 2 * Lo::kA) + Lo::kC);
+            mbar_expect_tx(bar, kStates ? Lo::kA : 2 * Lo::kA);
 #pragma unroll
-                for (int x = 0; x < DA / 64; ++x) tma_load_4d(at + Lo::kB + x * C * 128, &p.map[ps.mb], bar, 64 * x, un.h / ps.sb, t0, un.b);
-#pragma unroll
-                for (int x = 0; x < DC / 64; ++x) tma_load_4d(at + Lo::kCat + x * C * 128, &p.map[ps.mc], bar, 64 * x, un.h / ps.sc, t0, un.b);
-            }
-            __syncwarp();
-            if (kStates) continue;
-            if (g >= 2 && !wait_warp(mi, B_EMPTYA + st, (g >> 1) - 1)) return;     // the output staged there is on its way
-            if (elect_one())
+            for (int x = 0; x < DA / 64; ++x) tma_load_4d(at + Lo::kA + x * C * 128, &p.map[ps.mb], bar, 64 * x, un.h / ps.sb, t0, un.b);
+            if (!kStates)
 #pragma unroll
                 for (int x = 0; x < DA / 64; ++x) tma_load_4d(at + x * C * 128, &p.map[ps.ma], bar, 64 * x, un.h / ps.sa, t0, un.b);
-            __syncwarp();
         }
+        __syncwarp();
+        if (g >= 2 && !wait_warp(mi, kStates ? B_EMPTY + st : B_EMPTYC + st, (g >> 1) - 1)) return;     // the output staged there is on its way
+        if (elect_one()) {
+            unsigned long long *bar = &mi.bars[B_FULLC + st];
+            mbar_expect_tx(bar, Lo::kC);
+#pragma unroll
+            for (int x = 0; x < DC / 64; ++x) tma_load_4d(at + Lo::kCat + x * C * 128, &p.map[ps.mc], bar, 64 * x, un.h / ps.sc, t0, un.b);
+        }
+        __syncwarp();
     }
 }
 
@@ -223,71 +268,60 @@ template <int DA, int DC, bool kStates>
 __device__ __forceinline__ void run_mma(unsigned char *smem, Misc &mi, const Params &p, uint32_t tmem)
 {
     using Lo = Layout<DA, DC>;
-    const uint32_t tA = tmem, tU = tmem + 128, tO1 = tmem + 256, tO2 = tmem + 384;
+    const uint32_t tA = tmem + kColA, tU = tmem + kColU, tO = tmem + kColO, tK = tmem + kColK;
     const uint32_t base = smem_u32(smem);
-    constexpr uint32_t kIdA = idesc(C, 0), kIdQS = idesc(DC, 0) | kMnB, kIdKV = idesc(DC, 0) | kMnA | kMnB;
-    // DA = 64: the second 64 rows of U repeat the first
-    constexpr uint32_t kLdK = DA == 128 ? C * 128 : 0, kLdC = C * 128, kLdS = DA * 128;
+    constexpr uint32_t kIdA = idesc(C, 0), kIdC = idesc(DC, 0) | kMnB;
+    constexpr uint32_t kLdC = C * 128, kLdS = DA * 128;
     const uint32_t ss = desc_mn(base + Lo::kS, kLdS);
-    int g = 0;
-    for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
-        const Unit un(p, u, kStates);
-        for (int i = 0; i < un.hi - un.lo; ++i, ++g) {
-            const int st = g & 1;
-            const uint32_t at = base + st * Lo::kStage;
-            const uint32_t a = desc_k(at), b = desc_k(at + Lo::kB), key = desc_mn(at + Lo::kB, kLdK), c = desc_mn(at + Lo::kCat, kLdC);
+    int g = 0, parts = 0;                      // chunks so far, and those whose a S is multiplied by e
+    for (Cursor cur(p, kStates); cur.u < p.units; cur.next(p), ++g) {
+        const int st = g & 1;
+        const uint32_t at = base + st * Lo::kStage;
+        const uint32_t a = desc_k(at), b = desc_k(at + Lo::kA), c = desc_mn(at + Lo::kCat, kLdC);
+        if (!kStates) {
             if (!wait_warp(mi, B_FULL + st, g >> 1)) return;
-            if (!kStates) {
-                tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < DA / 16; ++k) mma_ss2(tA, a + step_k(k), kDescHi, b + step_k(k), kDescHi, kIdA, k > 0);
-                    mma_commit(&mi.bars[B_A]);
-                }
-                __syncwarp();
-            }
-            if (!wait_warp(mi, B_S, g)) return;
-            if (!kStates && g > 0 && !wait_warp(mi, B_OFREE, g - 1)) return;
-            tc_fence_after();
-            if (!kStates) {
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < DA / 16; ++k) mma_ss2(tO1, a + step_k(k), kDescHi, ss + k * kStepMn, kDescHi, kIdQS, k > 0);
-                }
-                __syncwarp();
-            }
-            if (!wait_warp(mi, B_KHI, g)) return;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < C / 16; ++k) mma_ss2(tU, key + k * kStepMn, kDescHi, c + k * kStepMn, kDescHi, kIdKV, k > 0);
-                mma_commit(&mi.bars[B_KV]);
+                for (int k = 0; k < DA / 16; ++k) mma_ss2(tA, a + step_k(k), kDescHi, b + step_k(k), kDescHi, kIdA, k > 0);
+                mma_commit(&mi.bars[B_A]);
             }
             __syncwarp();
-            if (!kStates) {
-                if (!wait_warp(mi, B_P, g)) return;
-                tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < C / 16; ++k) mma_ts2(tO2, tA + (k >> 2) * 64 + (k & 3) * 8, c + k * kStepMn, kDescHi, kIdQS, k > 0);
-                    mma_commit(&mi.bars[B_O]);
-                }
-                __syncwarp();
-            }
-            if (!wait_warp(mi, B_KLO, g)) return;
+        }
+        if (!wait_warp(mi, B_S, g)) return;                      // S is there, and U is read
+        if (!kStates) {
+            if (g > 0 && !wait_warp(mi, B_OFREE, g - 1)) return;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < C / 16; ++k) mma_ss2(tU, key + k * kStepMn, kDescHi, c + k * kStepMn, kDescHi, kIdKV, 1);
-                mma_commit(&mi.bars[B_U]);
-                mma_commit(&mi.bars[B_EMPTY + st]);
+                for (int k = 0; k < DA / 16; ++k) mma_ss2(tO, a + step_k(k), kDescHi, ss + k * kStepMn, kDescHi, kIdC, k > 0);
+                mma_commit(&mi.bars[B_QS]);
+            }
+            __syncwarp();
+        }
+        if (!wait_warp(mi, B_FULLC + st, g >> 1) || !wait_warp(mi, B_K, g)) return;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 2 * C / 16; ++k) mma_ts2(tU, tK + 8 * k, c + (k & (C / 16 - 1)) * kStepMn, kDescHi, kIdC, k > 0);
+            mma_commit(&mi.bars[B_U]);
+            mma_commit(&mi.bars[B_EMPTY + st]);
+        }
+        __syncwarp();
+        if (!kStates) {
+            if (!wait_warp(mi, B_P, g) || (!shares(p.log_decay[cur.un.h], p.pass[cur.un.pass]) && !wait_warp(mi, B_E, parts++))) return;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < C / 16; ++k) mma_ts2(tO, tA + (k >> 2) * 64 + (k & 3) * 8, c + k * kStepMn, kDescHi, kIdC, 1);
+                mma_commit(&mi.bars[B_O]);
             }
             __syncwarp();
         }
     }
 }
 
-// Outputs leave through the place of a and a tensor copy (32 rows of a warp's own stores lie in 32 different lines, which cost
+// Outputs leave through the place of c and a tensor copy (32 rows of a warp's own stores lie in 32 different lines, which cost
 // 4000 of 7300 cycles of a chunk); not those in fp32, which have no room there, nor a sequence's last rows where other rows follow
 // that have to stay as they are.
 __device__ __forceinline__ bool store_directly(const Params &p, const Pass &ps, int t0, int n) { return ps.out_f32 || (n < C && t0 + n < p.T); }
@@ -300,7 +334,7 @@ __device__ __forceinline__ void run_p(unsigned char *smem, Misc &mi, const Param
     const uint32_t lane = tmem + ((uint32_t)(w * 32) << 16);
     // the half's P goes over the half's own part of A, which its threads have read by then
     const uint32_t base = smem_u32(smem);
-    const uint32_t tA = lane + 64 * half, tO1 = lane + 256 + (DC / 2) * half, tO2 = tO1 + 128;
+    const uint32_t tA = lane + kColA + 64 * half, tO = lane + kColO + (DC / 2) * half;
     bool live = true;                          // after a wait that ran out a warp only keeps the group's barriers company
     int g = 0, nth = 0;                        // chunks and units with chunks so far
     for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
@@ -309,89 +343,113 @@ __device__ __forceinline__ void run_p(unsigned char *smem, Misc &mi, const Param
         const bool rev = ps.reverse != 0;
         const float ld = p.log_decay[un.h];
         if (un.hi == un.lo) continue;
-        const int set = nth++ & (kSets - 1);
+        const int set = nth++ % kSets;
         group_sync(1, 256);                    // the tables' readers are done with the last unit's
-        // forward: pw[31 + m], m = t - i from -31 to 127; reverse: pw[127 + m], m from -127 to 31
-        if (id < 31 + C) mi.pw[id] = (rev ? id > C - 1 : id < 31) ? 0.f : ps.sp * power(ld, rev ? C - 1 - id : id - 31);
-        const float *pw = mi.pw + (rev ? C - 1 : 31);
+        // Shared accumulator: pw[i] is the factor of column i.  Otherwise of distance m = t - i, forward at pw[31 + m] (m from -31 to
+        // 127), reverse at pw[127 + m] (-127 to 31).
+        const bool one = shares(ld, ps);
+        if (id < 31 + C) {
+            if (one) mi.pw[id] = ps.sp / ps.se * expf((float)(rev ? id - C + 1 : -(id + 1)) * ld);
+            else mi.pw[id] = (rev ? id > C - 1 : id < 31) ? 0.f : ps.sp * power(ld, rev ? C - 1 - id : id - 31);
+        }
+        const float *pw = mi.pw + (one ? 0 : rev ? C - 1 : 31);
         const float e_full = ps.se * power(ld, rev ? C - 1 - t : t + 1);
         group_sync(1, 256);
         for (int i = 0; i < un.hi - un.lo; ++i, ++g) {
             const int t0 = un.chunk(p, i) * C, n = min(C, un.len - t0);
             if (!(live = live && wait_warp(mi, B_A, g))) continue;
             tc_fence_after();
-            // One loop for blocks on and off the diagonal, with the power of each entry from the table: the kernel's code is
-            // read from the instruction cache by warps of four roles at once, and less of it was worth more than fewer loads.
+            // a reverse pass starts at the end of a sequence, where its distance to the chunk's end is shorter
+            const float short_of = one && rev && n < C ? expf((float)(C - n) * ld) : 1.f;
 #pragma unroll 1
             for (int x = 0; x < 2; ++x) {
-                const int j = 2 * half + x, m = t - 32 * j;        // the block of 32 tokens; the distance to its first
+                const int j = 2 * half + x, m = t - 32 * j;            // the block of 32 tokens; the distance to its first
                 uint32_t y[16];
 #pragma unroll
                 for (int z = 0; z < 16; ++z) y[z] = 0;
                 if (rev ? j >= w : j <= w) {
                     float v[32];
                     tmem_ld<32>(tA + 32 * x, reinterpret_cast<uint32_t *>(v));
-                    const float *d = pw + m;
-                    // tokens of the block that the row reads: z <= m, or m <= z < n - 32 j
-                    const int lo = rev ? max(m, 0) : 0, hi = rev ? min(n - 32 * j, 32) : min(m + 1, 32);
-                    const uint32_t keep = (hi <= lo ? 0u : 0xffffffffu >> (32 - hi)) & (lo > 31 ? 0u : 0xffffffffu << lo);
                     tc_wait_ld();
+                    if (short_of != 1.f)
 #pragma unroll
-                    for (int z = 0; z < 32; z += 2) {
-                        const float f0 = d[-z], f1 = d[-z - 1];
-                        const float q0 = v[z] * f0, q1 = v[z + 1] * f1;
-                        y[z / 2] = pack_bf16(keep & (1u << z) ? q0 : 0.f, keep & (2u << z) ? q1 : 0.f);
+                        for (int z = 0; z < 32; ++z) v[z] *= short_of;
+                    if (one) {
+#pragma unroll
+                        for (int z = 0; z < 32; z += 4) {
+                            const float4 c = *reinterpret_cast<const float4 *>(&mi.pw[32 * j + z]);
+                            y[z / 2] = pack2(mul2(two(v[z], v[z + 1]), two(c.x, c.y)));
+                            y[z / 2 + 1] = pack2(mul2(two(v[z + 2], v[z + 3]), two(c.z, c.w)));
+                        }
+                    } else {
+                        const float *d = pw + m;
+#pragma unroll
+                        for (int z = 0; z < 32; z += 2) y[z / 2] = pack_bf16(v[z] * d[-z], v[z + 1] * d[-z - 1]);
+                    }
+                    if (j == w || n < C) {
+                        // tokens of the block that the row reads: z <= m, or m <= z < n - 32 j
+                        const int lo = rev ? max(m, 0) : 0, hi = rev ? min(n - 32 * j, 32) : min(m + 1, 32);
+                        const uint32_t keep = (hi <= lo ? 0u : 0xffffffffu >> (32 - hi)) & (lo > 31 ? 0u : 0xffffffffu << lo);
+#pragma unroll
+                        for (int z = 0; z < 16; ++z) y[z] &= (keep >> (2 * z) & 1 ? 0xffffu : 0u) | (keep >> (2 * z) & 2 ? 0xffff0000u : 0u);
                     }
                 }
                 tmem_st16(tA + 16 * x, y);
             }
+            const float e = !one ? 1.f : rev && n < C ? ps.se * power(ld, max(n - 1 - t, 0)) : e_full;
             tc_wait_st();
             tc_fence_before();
             arrive(mi, B_P);
-            const float e = rev && n < C ? ps.se * power(ld, max(n - 1 - t, 0)) : e_full;
-            const uint64_t ee = two(e, e);
-            if (!(live = wait_warp(mi, B_O, g))) continue;     // (a S is done by then, and with it the last reading of a)
+            if (!(live = wait_warp(mi, B_O, g))) continue;     // (every product of the chunk is done)
             tc_fence_after();
             const bool bad = mi.any[set] != 0, direct = store_directly(p, ps, t0, n);
-            const int order = rev ? un.len - 1 - (t0 + t) : t0 + t;
-            const uint32_t stage = base + (g & 1) * Layout<DA, DC>::kStage;
+            const uint32_t stage = base + (g & 1) * Layout<DA, DC>::kStage + Layout<DA, DC>::kCat;
+            const uint64_t ee = two(e, e);
+            if (!bad && !direct) {
 #pragma unroll 1
-            for (int j = 0; j < DC / 2; j += 16) {
-                const int col = (DC / 2) * half + j;
-                float v[16], s[16];
-                tmem_ld<16>(tO1 + j, reinterpret_cast<uint32_t *>(s));
-                tmem_ld<16>(tO2 + j, reinterpret_cast<uint32_t *>(v));
-                tc_wait_ld();
-#pragma unroll
-                for (int x = 0; x < 16; x += 2) apart(fma2(ee, two(s[x], s[x + 1]), two(v[x], v[x + 1])), v[x], v[x + 1]);
-                if (bad) {
-#pragma unroll
-                    for (int x = 0; x < 16; ++x)
-                        if (order >= mi.first[set][col + x]) v[x] = __int_as_float(0x7fffffff);
-                }
-                if (direct && ps.out_f32) {
-                    float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(ps.out) + (((size_t)un.b * p.T + t0 + t) * p.H + un.h) * DC + col);
-                    if (t < n)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) o[x] = make_float4(v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]);
-                    continue;
-                }
-                uint32_t y[8];
-#pragma unroll
-                for (int x = 0; x < 8; ++x) y[x] = pack_bf16(v[2 * x], v[2 * x + 1]);
-                if (!direct) {
+                for (int j = 0; j < DC / 2; j += 32) {
+                    const int col = (DC / 2) * half + j;
                     const uint32_t at = stage + (col >> 6) * C * 128;
-                    sts128(at + sw_off(t, col & 63), y[0], y[1], y[2], y[3]);
-                    sts128(at + sw_off(t, (col & 63) + 8), y[4], y[5], y[6], y[7]);
-                } else if (t < n) {
-                    uint4 *o = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(ps.out) + (((size_t)un.b * p.T + t0 + t) * p.H + un.h) * DC + col);
-                    o[0] = make_uint4(y[0], y[1], y[2], y[3]);
-                    o[1] = make_uint4(y[4], y[5], y[6], y[7]);
+                    float v[32];
+                    tmem_ld<32>(tO + j, reinterpret_cast<uint32_t *>(v));
+                    tc_wait_ld();
+#pragma unroll
+                    for (int x = 0; x < 32; x += 8)
+                        sts128(at + sw_off(t, (col & 63) + x), pack2(mul2(ee, two(v[x], v[x + 1]))), pack2(mul2(ee, two(v[x + 2], v[x + 3]))),
+                               pack2(mul2(ee, two(v[x + 4], v[x + 5]))), pack2(mul2(ee, two(v[x + 6], v[x + 7]))));
+                }
+            } else {
+                const int order = rev ? un.len - 1 - (t0 + t) : t0 + t;
+#pragma unroll 1
+                for (int j = 0; j < DC / 2; j += 8) {
+                    const int col = (DC / 2) * half + j;
+                    float v[8];
+                    tmem_ld8(tO + j, reinterpret_cast<uint32_t *>(v));
+                    tc_wait_ld();
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        v[x] *= e;
+                        if (bad && order >= mi.first[set][col + x]) v[x] = __int_as_float(0x7fffffff);
+                    }
+                    const uint4 y = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+                    const size_t out = (((size_t)un.b * p.T + t0 + t) * p.H + un.h) * DC + col;
+                    if (!direct) {
+                        sts128(stage + (col >> 6) * C * 128 + sw_off(t, col & 63), y.x, y.y, y.z, y.w);
+                    } else if (t < n && ps.out_f32) {
+                        float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(ps.out) + out);
+                        o[0] = make_float4(v[0], v[1], v[2], v[3]);
+                        o[1] = make_float4(v[4], v[5], v[6], v[7]);
+                    } else if (t < n) {
+                        *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(ps.out) + out) = y;
+                    }
                 }
             }
             tc_fence_before();
             arrive(mi, B_OFREE);
             if (!direct) fence_async_smem();
+            // (A barrier's next completion must not come before everybody has seen the last one: the copying warp has when it has
+            // passed on the place of the chunk before.)
+            if (g > 0 && !(live = wait_warp(mi, B_EMPTYC + ((g - 1) & 1), (g - 1) >> 1))) continue;
             arrive(mi, B_OUT);
         }
     }
@@ -412,11 +470,12 @@ __device__ __forceinline__ void run_out(unsigned char *smem, Misc &mi, const Par
                 if (!store_directly(p, ps, t0, n)) {
 #pragma unroll
                     for (int x = 0; x < DC / 64; ++x)
-                        tma_store_4d(&p.out[un.pass], smem + (g & 1) * Layout<DA, DC>::kStage + x * C * 128, 64 * x, un.h, t0, un.b);
+                        tma_store_4d(&p.out[un.pass], smem + (g & 1) * Layout<DA, DC>::kStage + Layout<DA, DC>::kCat + x * C * 128, 64 * x,
+                                     un.h, t0, un.b);
                     tma_store_commit();
                     tma_store_wait_read();
                 }
-                arrive(mi, B_EMPTYA + (g & 1));
+                arrive(mi, B_EMPTYC + (g & 1));
             }
             __syncwarp();
         }
@@ -431,13 +490,14 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
     constexpr int N = DC / 2;                  // columns of a thread
     const int id = threadIdx.x - kWarpS * 32, k = id & 127, c0 = (id >> 7) * N;
     const bool mine = k < DA;
-    const uint32_t tU = tmem + 128 + c0 + ((uint32_t)(k & 96) << 16);
+    const uint32_t tU = tmem + kColU + c0 + ((uint32_t)(k & 96) << 16), tO = tmem + kColO + c0 + ((uint32_t)(k & 96) << 16);
     const uint32_t ss = smem_u32(smem) + Lo::kS;
     int g = 0, nth = 0;                        // chunks and units with chunks so far
     for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
         const Unit un(p, u, kStates);
         const Pass &ps = p.pass[un.pass];
         const float ld = p.log_decay[un.h];
+        const bool rev = ps.reverse != 0, one = kStates || shares(ld, ps);
         uint64_t s[N / 2];                     // two columns each
 #pragma unroll
         for (int x = 0; x < N / 2; ++x) s[x] = 0;
@@ -509,11 +569,30 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
             }
             if (!kStates) fence_async_smem();
             arrive(mi, B_S);
+            if (!kStates && !one) {
+                // e o (a S) in the accumulator, for heads where P c cannot be added to a S as it is
+                const int n = min(C, un.len - un.chunk(p, i) * C);
+                const float e = ps.se * power(ld, rev ? max(n - 1 - k, 0) : k + 1);
+                if (!wait_warp(mi, B_QS, g)) return;
+                tc_fence_after();
+#pragma unroll 1
+                for (int x = 0; x < N; x += 8) {
+                    uint32_t v[8];
+                    tmem_ld8(tO + x, v);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int y = 0; y < 8; ++y) v[y] = __float_as_uint(e * __uint_as_float(v[y]));
+                    tmem_st8(tO + x, v);
+                }
+                tc_wait_st();
+                tc_fence_before();
+                arrive(mi, B_E);
+            }
         }
         float *to = kStates ? ps.seg + ((size_t)un.pair * (p.nseg - 1) + un.seg) * DA * DC
                             : un.seg == p.nseg - 1 && ps.s_out ? ps.s_out + (size_t)un.pair * DA * DC : nullptr;
         if (to && mine) {
-            const int set = (nth - 1) & (kSets - 1);
+            const int set = (nth - 1) % kSets;
             const bool bad = chunks > 0 && mi.any[set];
 #pragma unroll
             for (int x = 0; x < N; x += 4) {
@@ -531,16 +610,19 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
     }
 }
 
-// w o b in two parts, and c made safe: a thread has token r of the chunk and one half of the channels
+// w o b in two parts, and c made safe.  A warp has 32 channels of b (its tensor memory lanes) and 64 tokens: 8 x 8 blocks come
+// transposed out of shared memory in the fragment that the 16-lane stores of tensor memory take, so the product's operand never
+// goes back through shared memory, whose bandwidth the other products need.
 template <int DA, int DC, bool kStates>
-__device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Params &p)
+__device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Params &p, uint32_t tmem)
 {
     using Lo = Layout<DA, DC>;
-    constexpr int NA = DA / 2, NC = DC / 2;
-    const int id = threadIdx.x - kWarpK * 32, r = id & 127, half = id >> 7;
+    constexpr int NC = DC / 2;
+    const int id = threadIdx.x - kWarpK * 32, lane = id & 31, quad = (id >> 5) & 3, half = id >> 7, r = id & 127;
     const uint32_t base = smem_u32(smem);
-    // byte offset of channel `ch` (a multiple of 8) of the thread's token in a tile
-    const auto off = [r](int ch) { return (ch >> 6) * C * 128 + sw_off(r, ch & 63); };
+    const uint32_t tK = tmem + kColK + 32 * half + ((uint32_t)(quad * 32) << 16);
+    const bool mine = 32 * quad < DA;
+    const int tok0 = 64 * half + 2 * (lane & 3);               // the thread's tokens: tok0 + 8 i, and the next
     bool live = true;                          // as in run_p
     int g = 0, nth = 0;                        // chunks and units with chunks so far
     for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
@@ -550,16 +632,74 @@ __device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Pa
         const float ld = p.log_decay[un.h];
         const int chunks = un.hi - un.lo;
         if (chunks == 0) continue;
-        const int set = nth++ & (kSets - 1);
+        const int set = nth++ % kSets;
         if (half == 0) mi.first[set][r] = kNever;
         if (id == 0) mi.any[set] = 0;
         group_sync(2, 256);
+        uint64_t w[8];
+        int weights_of = -1;                   // the chunk length that w is for
         for (int i = 0; i < chunks; ++i, ++g) {
             const int st = g & 1, t0 = un.chunk(p, i) * C, n = min(C, un.len - t0);
-            const uint32_t sb = base + st * Lo::kStage + Lo::kB, sc = base + st * Lo::kStage + Lo::kCat;
-            const int hops = rev ? r + 1 : n - 1 - r;
-            const float w = ps.sw * power(ld, max(hops, 0));
-            if (!(live = live && wait_warp(mi, B_FULL + st, g >> 1))) continue;
+            const uint32_t sb = base + st * Lo::kStage + Lo::kA, sc = base + st * Lo::kStage + Lo::kCat;
+            if (n != weights_of) {
+                weights_of = n;
+#pragma unroll 1
+                for (int x = 0; x < 16; ++x) {
+                    const int tok = tok0 + 8 * (x >> 1) + (x & 1), hops = rev ? tok + 1 : n - 1 - tok;
+                    const float f = tok < n ? ps.sw * power(ld, hops) : 0.f;
+#pragma unroll
+                    for (int y = 0; y < 8; ++y) {              // (registers have no index)
+                        float w0, w1;
+                        apart(w[y], w0, w1);
+                        if (2 * y == x) w[y] = two(f, 0.f);
+                        if (2 * y + 1 == x) w[y] = two(w0, f);
+                    }
+                }
+            }
+            const auto off = [r](int ch) { return (uint32_t)((ch >> 6) * C * 128 + sw_off(r, ch & 63)); };
+            live = live && wait_warp(mi, B_FULL + st, g >> 1) && (g == 0 || wait_warp(mi, B_U, g - 1));
+            if (n < C) {                       // tokens behind the end: whatever is there is no value
+                live = live && wait_warp(mi, B_FULLC + st, g >> 1);
+                if (live && r >= n) {
+#pragma unroll 1
+                    for (int x = 0; x < DA / 2; x += 8) sts128(sb + off(half * (DA / 2) + x), 0, 0, 0, 0);
+#pragma unroll 1
+                    for (int x = 0; x < NC; x += 8) sts128(sc + off(half * NC + x), 0, 0, 0, 0);
+                    fence_async_smem();
+                }
+                group_sync(2, 256);
+            }
+            if (!live) continue;
+            tc_fence_after();
+            if (mine) {
+                const uint64_t minus = two(-1.f, -1.f);
+#pragma unroll 1
+                for (int rows = 0; rows < 32; rows += 16) {
+                    const int ch = 32 * quad + rows + 8 * ((lane >> 3) & 1);
+                    const uint32_t from = sb + (ch >> 6) * C * 128;
+#pragma unroll
+                    for (int x = 0; x < 8; x += 4) {           // blocks of 8 tokens
+                        uint32_t hi[8], lo[8];
+#pragma unroll
+                        for (int z = 0; z < 4; z += 2) {
+                            const int tok = 64 * half + 8 * (x + z + (lane >> 4)) + (lane & 7);
+                            uint32_t v[4];
+                            ldmatrix_x4_trans(v, from + sw_off(tok, ch & 63));
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                const uint64_t f = mul2(unpack2(v[y]), w[x + z + (y >> 1)]);
+                                hi[2 * z + y] = pack2(f);
+                                lo[2 * z + y] = pack2(fma2(unpack2(hi[2 * z + y]), minus, f));
+                            }
+                        }
+                        tmem_st_16x128b_x4(tK + 4 * x + ((uint32_t)rows << 16), hi);
+                        tmem_st_16x128b_x4(tK + 64 + 4 * x + ((uint32_t)rows << 16), lo);
+                    }
+                }
+                tc_wait_st();
+            }
+            tc_fence_before();
+            if (!(live = wait_warp(mi, B_FULLC + st, g >> 1))) continue;
             uint32_t odd = 0;
 #pragma unroll
             for (int x = 0; x < NC; x += 8) {
@@ -567,10 +707,7 @@ __device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Pa
                 odd |= ((v.x & 0x7fff7fffu) + 0x00800080u) | ((v.y & 0x7fff7fffu) + 0x00800080u) | ((v.z & 0x7fff7fffu) + 0x00800080u) |
                        ((v.w & 0x7fff7fffu) + 0x00800080u);
             }
-            if (r >= n) {                      // behind the end: whatever is there is no value
-#pragma unroll 1
-                for (int x = 0; x < NC; x += 8) sts128(sc + off(half * NC + x), 0, 0, 0, 0);
-            } else if (odd & 0x80008000u) {
+            if (odd & 0x80008000u) {
 #pragma unroll 1
                 for (int x = half * NC; x < (half + 1) * NC; ++x) {
                     const uint32_t at = sc + off(x);
@@ -580,38 +717,9 @@ __device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Pa
                         mi.any[set] = 1;
                     }
                 }
+                fence_async_smem();
             }
-            if (!kStates && !(live = wait_warp(mi, B_A, g))) continue;
-            uint32_t lo[NA / 2];
-            if (r < n) {
-                const uint64_t ww = two(w, w), minus = two(-1.f, -1.f);
-#pragma unroll
-                for (int x = 0; x < NA; x += 8) {
-                    const uint32_t at = sb + off(half * NA + x);
-                    const uint4 v = lds128(at);
-                    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-                    uint32_t hi[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const uint64_t f = mul2(unpack2(in[y]), ww);
-                        hi[y] = pack2(f);
-                        lo[x / 2 + y] = pack2(fma2(unpack2(hi[y]), minus, f));
-                    }
-                    sts128(at, hi[0], hi[1], hi[2], hi[3]);
-                }
-            } else {
-#pragma unroll
-                for (int x = 0; x < NA / 2; ++x) lo[x] = 0;
-#pragma unroll
-                for (int x = 0; x < NA; x += 8) sts128(sb + off(half * NA + x), 0, 0, 0, 0);
-            }
-            fence_async_smem();
-            arrive(mi, B_KHI);
-            if (!(live = wait_warp(mi, B_KV, g))) continue;
-#pragma unroll
-            for (int x = 0; x < NA; x += 8) sts128(sb + off(half * NA + x), lo[x / 2], lo[x / 2 + 1], lo[x / 2 + 2], lo[x / 2 + 3]);
-            fence_async_smem();
-            arrive(mi, B_KLO);
+            arrive(mi, B_K);
         }
     }
 }
@@ -623,7 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1) sfda_linear_tc_kernel(const __gri
     Misc &mi = *reinterpret_cast<Misc *>(smem + Layout<DA, DC>::kMisc);
     const int tid = threadIdx.x, warp = tid >> 5;
     if (tid == 0) {
-        const int counts[kBars] = {1, 1, 1, 1, 1, 1, 1, 256, 1, 256, 256, 1, 256, 256, 256, 1};
+        const int counts[kBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 256, 1, 256, 1, 256, 256, 256, 256};
         for (int i = 0; i < kBars; ++i) mbar_init(&mi.bars[i], counts[i]);
         mi.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -644,7 +752,7 @@ __global__ void __launch_bounds__(kThreads, 1) sfda_linear_tc_kernel(const __gri
         if (warp == 2 && !kStates) run_out<DA, DC>(smem, mi, p);
     } else if (warp >= kWarpK) {
         regs_dec<kRegsK>();
-        run_keys<DA, DC, kStates>(smem, mi, p);
+        run_keys<DA, DC, kStates>(smem, mi, p, tmem);
     } else if (warp >= kWarpS) {
         regs_inc<kRegsS>();
         run_state<DA, DC, kStates>(smem, mi, p, tmem);
