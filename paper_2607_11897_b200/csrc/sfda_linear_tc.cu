@@ -16,7 +16,7 @@
 //
 // Bound by memory (a, b, c read once, out written once).  28 warps: TMA, MMA, output copies, one idle, eight each for P and the output, for the
 // state and for w o b.  Two stages of (a, b, c); the high part of w o b replaces b and the low part that, once the products that
-// read them are done, and the output leaves through the place of c.
+// read them are done, and 
 #include <cuda.h>
 
 #include "sfda_common.cuh"
@@ -41,7 +41,7 @@ static_assert(kRegsCtrl + 2 * (kRegsP + kRegsS + kRegsK) <= 7 * kRegsLaunch, "se
 // tensor memory: A (and P over it), U, O, the two parts of w o b
 constexpr uint32_t kColA = 0, kColU = 128, kColO = 256, kColK = 384;
 
-enum { B_FULL = 0, B_FULLC = 2, B_EMPTY = 4, B_EMPTYC = 6, B_A = 8, B_QS, B_K, B_U, B_P, B_O, B_OFREE, B_OUT, B_S, B_E, kBars };
+enum { B_FULL = 0, B_EMPTY = 2, B_FULLA = 4, B_EMPTYA, B_EMPTYO, B_A, B_QS, B_K, B_U, B_P, B_O, B_OFREE, B_OUT, B_S, B_E, kBars };
 
 struct Pass {
     void *out;
@@ -62,12 +62,11 @@ struct alignas(64) Params {
     int n_pass, T, H, pairs, nseg, cps, units, clear;     // cps: chunks of a stretch; clear: the call's first launch
 };
 
-// Shared memory: two stages of a, b, c and the bf16 state, then the small things.
+// Shared memory: a, two stages of b and c, the bf16 state, the output on its way out, then the small things.
 template <int DA, int DC>
 struct Layout {
-    static constexpr int kA = C * DA * 2, kC = C * DC * 2;
-    static constexpr int kCat = 2 * kA, kStage = kCat + kC;      // a, b, c
-    static constexpr int kS = 2 * kStage, kMisc = kS + DA * DC * 2;
+    static constexpr int kA = C * DA * 2, kC = C * DC * 2, kStage = kA + kC;
+    static constexpr int kS = kA + 2 * kStage, kOut = kS + DA * DC * 2, kMisc = kOut + kC;
 };
 struct Misc {
     unsigned long long bars[kBars];
@@ -103,6 +102,16 @@ __device__ __forceinline__ bool wait_warp(Misc &mi, int bar, int k)
     }
     mi.abort = 1;
     return false;
+}
+// whether it has come already
+__device__ __forceinline__ bool ready(Misc &mi, int bar, int k)
+{
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok)
+                 : "r"(smem_u32(&mi.bars[bar])), "r"((uint32_t)k & 1u)
+                 : "memory");
+    return __all_sync(0xffffffffu, ok) != 0;
 }
 __device__ __forceinline__ void arrive(Misc &mi, int bar)
 {
@@ -161,7 +170,27 @@ __device__ __forceinline__ uint32_t pack2(uint64_t v)
     apart(v, x, y);
     return pack_bf16(x, y);
 }
-__device__ __forceinline__ uint64_t unpack2(uint32_t w) { return two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+// the larger magnitudes; not finite once one of them is not
+__device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("{\n.reg .b32 x;\nabs.bf16x2 x, %1;\nmax.NaN.bf16x2 %0, x, %2;\n}\n" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 __device__ __forceinline__ void group_sync(int id, int threads) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // Operand descriptors as two 32-bit halves, of which only the lower one moves along K: the issuing thread spends one addition of
@@ -232,35 +261,60 @@ struct Cursor {
     __device__ __forceinline__ void next(const Params &p) { ++i; skip(p); }
 };
 
+__device__ __forceinline__ void prefetch_4d(const CUtensorMap *map, int c0, int c1, int c2, int c3)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1),
+                 "r"(c2), "r"(c3)
+                 : "memory");
+}
+
+// b and c of a chunk are loaded a chunk ahead.  a has one place, which is free from a S on: it is loaded then, out of L2, where it
+// was asked for together with b and c.
 template <int DA, int DC, bool kStates>
 __device__ __forceinline__ void run_tma(unsigned char *smem, Misc &mi, const Params &p)
 {
     using Lo = Layout<DA, DC>;
-    int g = 0;
-    for (Cursor cur(p, kStates); cur.u < p.units; cur.next(p), ++g) {
-        const Unit &un = cur.un;
+    Cursor next(p, kStates);                   // whose b and c are loaded
+    int gn = 0;
+    const auto load_bc = [&]() -> bool {
+        if (next.u >= p.units) return true;
+        const Unit &un = next.un;
         const Pass &ps = p.pass[un.pass];
-        const int st = g & 1, t0 = un.chunk(p, cur.i) * C;
-        unsigned char *at = smem + st * Lo::kStage;
-        if (g >= 2 && !wait_warp(mi, B_EMPTY + st, (g >> 1) - 1)) return;
+        const int st = gn & 1, t0 = un.chunk(p, next.i) * C;
+        unsigned char *at = smem + Lo::kA + st * Lo::kStage;
+        if (gn >= 2 && !wait_warp(mi, B_EMPTY + st, (gn >> 1) - 1)) return false;
         if (elect_one()) {
             unsigned long long *bar = &mi.bars[B_FULL + st];
-            mbar_expect_tx(bar, kStates ? Lo::kA : 2 * Lo::kA);
+            mbar_expect_tx(bar, Lo::kStage);
 #pragma unroll
-            for (int x = 0; x < DA / 64; ++x) tma_load_4d(at + Lo::kA + x * C * 128, &p.map[ps.mb], bar, 64 * x, un.h / ps.sb, t0, un.b);
+            for (int x = 0; x < DA / 64; ++x) tma_load_4d(at + x * C * 128, &p.map[ps.mb], bar, 64 * x, un.h / ps.sb, t0, un.b);
+#pragma unroll
+            for (int x = 0; x < DC / 64; ++x) tma_load_4d(at + Lo::kA + x * C * 128, &p.map[ps.mc], bar, 64 * x, un.h / ps.sc, t0, un.b);
             if (!kStates)
 #pragma unroll
-                for (int x = 0; x < DA / 64; ++x) tma_load_4d(at + x * C * 128, &p.map[ps.ma], bar, 64 * x, un.h / ps.sa, t0, un.b);
+                for (int x = 0; x < DA / 64; ++x) prefetch_4d(&p.map[ps.ma], 64 * x, un.h / ps.sa, t0, un.b);
         }
         __syncwarp();
-        if (g >= 2 && !wait_warp(mi, kStates ? B_EMPTY + st : B_EMPTYC + st, (g >> 1) - 1)) return;     // the output staged there is on its way
-        if (elect_one()) {
-            unsigned long long *bar = &mi.bars[B_FULLC + st];
-            mbar_expect_tx(bar, Lo::kC);
+        next.next(p);
+        ++gn;
+        return true;
+    };
+    if (!load_bc()) return;
+    int g = 0;
+    for (Cursor cur(p, kStates); cur.u < p.units; cur.next(p), ++g) {
+        if (!kStates) {
+            const Unit &un = cur.un;
+            const Pass &ps = p.pass[un.pass];
+            if (g >= 1 && !wait_warp(mi, B_EMPTYA, g - 1)) return;
+            if (elect_one()) {
+                unsigned long long *bar = &mi.bars[B_FULLA];
+                mbar_expect_tx(bar, Lo::kA);
 #pragma unroll
-            for (int x = 0; x < DC / 64; ++x) tma_load_4d(at + Lo::kCat + x * C * 128, &p.map[ps.mc], bar, 64 * x, un.h / ps.sc, t0, un.b);
+                for (int x = 0; x < DA / 64; ++x) tma_load_4d(smem + x * C * 128, &p.map[ps.ma], bar, 64 * x, un.h / ps.sa, un.chunk(p, cur.i) * C, un.b);
+            }
+            __syncwarp();
         }
-        __syncwarp();
+        if (!load_bc()) return;
     }
 }
 
@@ -276,10 +330,11 @@ __device__ __forceinline__ void run_mma(unsigned char *smem, Misc &mi, const Par
     int g = 0, parts = 0;                      // chunks so far, and those whose a S is multiplied by e
     for (Cursor cur(p, kStates); cur.u < p.units; cur.next(p), ++g) {
         const int st = g & 1;
-        const uint32_t at = base + st * Lo::kStage;
-        const uint32_t a = desc_k(at), b = desc_k(at + Lo::kA), c = desc_mn(at + Lo::kCat, kLdC);
+        const uint32_t at = base + Lo::kA + st * Lo::kStage;
+        const uint32_t a = desc_k(base), b = desc_k(at), c = desc_mn(at + Lo::kA, kLdC);
+        if (!wait_warp(mi, B_FULL + st, g >> 1)) return;
         if (!kStates) {
-            if (!wait_warp(mi, B_FULL + st, g >> 1)) return;
+            if (!wait_warp(mi, B_FULLA, g)) return;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
@@ -296,20 +351,27 @@ __device__ __forceinline__ void run_mma(unsigned char *smem, Misc &mi, const Par
 #pragma unroll
                 for (int k = 0; k < DA / 16; ++k) mma_ss2(tO, a + step_k(k), kDescHi, ss + k * kStepMn, kDescHi, kIdC, k > 0);
                 mma_commit(&mi.bars[B_QS]);
+                mma_commit(&mi.bars[B_EMPTYA]);
             }
             __syncwarp();
         }
-        if (!wait_warp(mi, B_FULLC + st, g >> 1) || !wait_warp(mi, B_K, g)) return;
-        tc_fence_after();
-        if (elect_one()) {
+        // U, and P c as soon as P is ready: the next a S waits for the state that takes U, and for the output to be read, which
+        // takes longer.  (B_K also says that c is safe.)
+        if (!wait_warp(mi, B_K, g)) return;
+        const bool one = kStates || shares(p.log_decay[cur.un.h], p.pass[cur.un.pass]);
+        bool u = kStates || !one || !ready(mi, B_P, g), o = kStates;
+        while (true) {
+            tc_fence_after();
+            if (u) {
+                if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < 2 * C / 16; ++k) mma_ts2(tU, tK + 8 * k, c + (k & (C / 16 - 1)) * kStepMn, kDescHi, kIdC, k > 0);
-            mma_commit(&mi.bars[B_U]);
-            mma_commit(&mi.bars[B_EMPTY + st]);
-        }
-        __syncwarp();
-        if (!kStates) {
-            if (!wait_warp(mi, B_P, g) || (!shares(p.log_decay[cur.un.h], p.pass[cur.un.pass]) && !wait_warp(mi, B_E, parts++))) return;
+                    for (int k = 0; k < 2 * C / 16; ++k) mma_ts2(tU, tK + 8 * k, c + (k & (C / 16 - 1)) * kStepMn, kDescHi, kIdC, k > 0);
+                    mma_commit(&mi.bars[B_U]);
+                }
+                __syncwarp();
+                if (o) break;
+            }
+            if (!wait_warp(mi, B_P, g) || (!one && !wait_warp(mi, B_E, parts++))) return;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
@@ -317,14 +379,78 @@ __device__ __forceinline__ void run_mma(unsigned char *smem, Misc &mi, const Par
                 mma_commit(&mi.bars[B_O]);
             }
             __syncwarp();
+            if (u) break;
+            u = o = true;
         }
+        if (elect_one()) mma_commit(&mi.bars[B_EMPTY + st]);
+        __syncwarp();
     }
 }
 
-// Outputs leave through the place of c and a tensor copy (32 rows of a warp's own stores lie in 32 different lines, which cost
+// Outputs leave through shared memory and a tensor copy (32 rows of a warp's own stores lie in 32 different lines, which cost
 // 4000 of 7300 cycles of a chunk); not those in fp32, which have no room there, nor a sequence's last rows where other rows follow
 // that have to stay as they are.
 __device__ __forceinline__ bool store_directly(const Params &p, const Pass &ps, int t0, int n) { return ps.out_f32 || (n < C && t0 + n < p.T); }
+
+// The output: a thread has row t of the chunk and one half of the columns.  False: a wait ran out.
+template <int DA, int DC>
+__device__ __forceinline__ bool write_out(unsigned char *smem, Misc &mi, const Params &p, uint32_t tmem, const Unit &un, int g, int t0, int n, int set, float e)
+{
+    const int id = threadIdx.x - kWarpP * 32, t = id & 127, half = id >> 7;
+    const uint32_t tO = tmem + kColO + (DC / 2) * half + ((uint32_t)(t & 96) << 16);
+    const Pass &ps = p.pass[un.pass];
+    if (!wait_warp(mi, B_O, g)) return false;                // (every product of the chunk is done)
+    tc_fence_after();
+    const bool bad = mi.any[set] != 0, direct = store_directly(p, ps, t0, n);
+    const uint32_t stage = smem_u32(smem) + Layout<DA, DC>::kOut;
+    // the place is free, and the copying warp has seen the last completion of B_OUT
+    if (g > 0 && !wait_warp(mi, B_EMPTYO, g - 1)) return false;
+    if (!bad && !direct) {
+        const uint64_t ee = two(e, e);
+#pragma unroll 1
+        for (int j = 0; j < DC / 2; j += 32) {
+            const int col = (DC / 2) * half + j;
+            const uint32_t at = stage + (col >> 6) * C * 128;
+            float v[32];
+            tmem_ld<32>(tO + j, reinterpret_cast<uint32_t *>(v));
+            tc_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 32; x += 8)
+                sts128(at + sw_off(t, (col & 63) + x), pack2(mul2(ee, two(v[x], v[x + 1]))), pack2(mul2(ee, two(v[x + 2], v[x + 3]))),
+                       pack2(mul2(ee, two(v[x + 4], v[x + 5]))), pack2(mul2(ee, two(v[x + 6], v[x + 7]))));
+        }
+    } else {
+        const int order = ps.reverse ? un.len - 1 - (t0 + t) : t0 + t;
+#pragma unroll 1
+        for (int j = 0; j < DC / 2; j += 8) {
+            const int col = (DC / 2) * half + j;
+            float v[8];
+            tmem_ld8(tO + j, reinterpret_cast<uint32_t *>(v));
+            tc_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                v[x] *= e;
+                if (bad && order >= mi.first[set][col + x]) v[x] = __int_as_float(0x7fffffff);
+            }
+            const uint4 y = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            const size_t out = (((size_t)un.b * p.T + t0 + t) * p.H + un.h) * DC + col;
+            if (!direct) {
+                sts128(stage + (col >> 6) * C * 128 + sw_off(t, col & 63), y.x, y.y, y.z, y.w);
+            } else if (t < n && ps.out_f32) {
+                float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(ps.out) + out);
+                o[0] = make_float4(v[0], v[1], v[2], v[3]);
+                o[1] = make_float4(v[4], v[5], v[6], v[7]);
+            } else if (t < n) {
+                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(ps.out) + out) = y;
+            }
+        }
+    }
+    tc_fence_before();
+    arrive(mi, B_OFREE);
+    if (!direct) fence_async_smem();
+    arrive(mi, B_OUT);
+    return true;
+}
 
 // P and the output: a thread has row t of the chunk and one half of the columns
 template <int DA, int DC>
@@ -333,8 +459,7 @@ __device__ __forceinline__ void run_p(unsigned char *smem, Misc &mi, const Param
     const int id = threadIdx.x - kWarpP * 32, t = id & 127, w = t >> 5, half = id >> 7;
     const uint32_t lane = tmem + ((uint32_t)(w * 32) << 16);
     // the half's P goes over the half's own part of A, which its threads have read by then
-    const uint32_t base = smem_u32(smem);
-    const uint32_t tA = lane + kColA + 64 * half, tO = lane + kColO + (DC / 2) * half;
+    const uint32_t tA = lane + kColA + 64 * half;
     bool live = true;                          // after a wait that ran out a warp only keeps the group's barriers company
     int g = 0, nth = 0;                        // chunks and units with chunks so far
     for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
@@ -344,6 +469,7 @@ __device__ __forceinline__ void run_p(unsigned char *smem, Misc &mi, const Param
         const float ld = p.log_decay[un.h];
         if (un.hi == un.lo) continue;
         const int set = nth++ % kSets;
+        const float e_full = !shares(ld, ps) ? 1.f : ps.se * power(ld, rev ? C - 1 - t : t + 1);
         group_sync(1, 256);                    // the tables' readers are done with the last unit's
         // Shared accumulator: pw[i] is the factor of column i.  Otherwise of distance m = t - i, forward at pw[31 + m] (m from -31 to
         // 127), reverse at pw[127 + m] (-127 to 31).
@@ -353,7 +479,6 @@ __device__ __forceinline__ void run_p(unsigned char *smem, Misc &mi, const Param
             else mi.pw[id] = (rev ? id > C - 1 : id < 31) ? 0.f : ps.sp * power(ld, rev ? C - 1 - id : id - 31);
         }
         const float *pw = mi.pw + (one ? 0 : rev ? C - 1 : 31);
-        const float e_full = ps.se * power(ld, rev ? C - 1 - t : t + 1);
         group_sync(1, 256);
         for (int i = 0; i < un.hi - un.lo; ++i, ++g) {
             const int t0 = un.chunk(p, i) * C, n = min(C, un.len - t0);
@@ -396,61 +521,10 @@ __device__ __forceinline__ void run_p(unsigned char *smem, Misc &mi, const Param
                 }
                 tmem_st16(tA + 16 * x, y);
             }
-            const float e = !one ? 1.f : rev && n < C ? ps.se * power(ld, max(n - 1 - t, 0)) : e_full;
             tc_wait_st();
             tc_fence_before();
             arrive(mi, B_P);
-            if (!(live = wait_warp(mi, B_O, g))) continue;     // (every product of the chunk is done)
-            tc_fence_after();
-            const bool bad = mi.any[set] != 0, direct = store_directly(p, ps, t0, n);
-            const uint32_t stage = base + (g & 1) * Layout<DA, DC>::kStage + Layout<DA, DC>::kCat;
-            const uint64_t ee = two(e, e);
-            if (!bad && !direct) {
-#pragma unroll 1
-                for (int j = 0; j < DC / 2; j += 32) {
-                    const int col = (DC / 2) * half + j;
-                    const uint32_t at = stage + (col >> 6) * C * 128;
-                    float v[32];
-                    tmem_ld<32>(tO + j, reinterpret_cast<uint32_t *>(v));
-                    tc_wait_ld();
-#pragma unroll
-                    for (int x = 0; x < 32; x += 8)
-                        sts128(at + sw_off(t, (col & 63) + x), pack2(mul2(ee, two(v[x], v[x + 1]))), pack2(mul2(ee, two(v[x + 2], v[x + 3]))),
-                               pack2(mul2(ee, two(v[x + 4], v[x + 5]))), pack2(mul2(ee, two(v[x + 6], v[x + 7]))));
-                }
-            } else {
-                const int order = rev ? un.len - 1 - (t0 + t) : t0 + t;
-#pragma unroll 1
-                for (int j = 0; j < DC / 2; j += 8) {
-                    const int col = (DC / 2) * half + j;
-                    float v[8];
-                    tmem_ld8(tO + j, reinterpret_cast<uint32_t *>(v));
-                    tc_wait_ld();
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        v[x] *= e;
-                        if (bad && order >= mi.first[set][col + x]) v[x] = __int_as_float(0x7fffffff);
-                    }
-                    const uint4 y = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-                    const size_t out = (((size_t)un.b * p.T + t0 + t) * p.H + un.h) * DC + col;
-                    if (!direct) {
-                        sts128(stage + (col >> 6) * C * 128 + sw_off(t, col & 63), y.x, y.y, y.z, y.w);
-                    } else if (t < n && ps.out_f32) {
-                        float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(ps.out) + out);
-                        o[0] = make_float4(v[0], v[1], v[2], v[3]);
-                        o[1] = make_float4(v[4], v[5], v[6], v[7]);
-                    } else if (t < n) {
-                        *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(ps.out) + out) = y;
-                    }
-                }
-            }
-            tc_fence_before();
-            arrive(mi, B_OFREE);
-            if (!direct) fence_async_smem();
-            // (A barrier's next completion must not come before everybody has seen the last one: the copying warp has when it has
-            // passed on the place of the chunk before.)
-            if (g > 0 && !(live = wait_warp(mi, B_EMPTYC + ((g - 1) & 1), (g - 1) >> 1))) continue;
-            arrive(mi, B_OUT);
+            live = write_out<DA, DC>(smem, mi, p, tmem, un, g, t0, n, set, one && rev && n < C ? ps.se * power(ld, max(n - 1 - t, 0)) : e_full);
         }
     }
 }
@@ -470,12 +544,11 @@ __device__ __forceinline__ void run_out(unsigned char *smem, Misc &mi, const Par
                 if (!store_directly(p, ps, t0, n)) {
 #pragma unroll
                     for (int x = 0; x < DC / 64; ++x)
-                        tma_store_4d(&p.out[un.pass], smem + (g & 1) * Layout<DA, DC>::kStage + Layout<DA, DC>::kCat + x * C * 128, 64 * x,
-                                     un.h, t0, un.b);
+                        tma_store_4d(&p.out[un.pass], smem + Layout<DA, DC>::kOut + x * C * 128, 64 * x, un.h, t0, un.b);
                     tma_store_commit();
                     tma_store_wait_read();
                 }
-                arrive(mi, B_EMPTYC + (g & 1));
+                arrive(mi, B_EMPTYO);
             }
             __syncwarp();
         }
@@ -542,7 +615,7 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
                 const bool weak = x0 > -0.5f;
                 const float gm = weak ? expm1f(x0) : expf(x0);
                 const uint64_t gg = two(gm, gm), one = weak ? two(1.f, 1.f) : 0;
-                if (!wait_warp(mi, B_U, g)) return;
+                if (!wait_warp(mi, B_U, g)) return;    // (and with it a S, the reader of S's copy)
                 tc_fence_after();
                 ++g;
 #pragma unroll
@@ -610,7 +683,8 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
     }
 }
 
-// w o b in two parts, and c made safe.  A warp has 32 channels of b (its tensor memory lanes) and 64 tokens: 8 x 8 blocks come
+// w o b in two parts, and c made safe.  With w = w1 + w2, both bf16, the high part is bf16(w1 b), and the low one b w2 plus what the
+// high one's rounding left, which a fused multiply-add gives exactly: three instructions for two elements.  A warp has 32 channels of b (its tensor memory lanes) and 64 tokens: 8 x 8 blocks come
 // transposed out of shared memory in the fragment that the 16-lane stores of tensor memory take, so the product's operand never
 // goes back through shared memory, whose bandwidth the other products need.
 template <int DA, int DC, bool kStates>
@@ -636,30 +710,28 @@ __device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Pa
         if (half == 0) mi.first[set][r] = kNever;
         if (id == 0) mi.any[set] = 0;
         group_sync(2, 256);
-        uint64_t w[8];
+        uint32_t w[8], wlo[8];                 // two tokens each: bf16(w) and bf16 of the rest
         int weights_of = -1;                   // the chunk length that w is for
         for (int i = 0; i < chunks; ++i, ++g) {
             const int st = g & 1, t0 = un.chunk(p, i) * C, n = min(C, un.len - t0);
-            const uint32_t sb = base + st * Lo::kStage + Lo::kA, sc = base + st * Lo::kStage + Lo::kCat;
+            const uint32_t sb = base + Lo::kA + st * Lo::kStage, sc = sb + Lo::kA;
             if (n != weights_of) {
                 weights_of = n;
-#pragma unroll 1
-                for (int x = 0; x < 16; ++x) {
-                    const int tok = tok0 + 8 * (x >> 1) + (x & 1), hops = rev ? tok + 1 : n - 1 - tok;
-                    const float f = tok < n ? ps.sw * power(ld, hops) : 0.f;
 #pragma unroll
-                    for (int y = 0; y < 8; ++y) {              // (registers have no index)
-                        float w0, w1;
-                        apart(w[y], w0, w1);
-                        if (2 * y == x) w[y] = two(f, 0.f);
-                        if (2 * y + 1 == x) w[y] = two(w0, f);
+                for (int x = 0; x < 8; ++x) {
+                    float f[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int tok = tok0 + 8 * x + y, hops = rev ? tok + 1 : n - 1 - tok;
+                        f[y] = tok < n ? ps.sw * power(ld, hops) : 0.f;
                     }
+                    w[x] = pack_bf16(f[0], f[1]);
+                    wlo[x] = pack_bf16(f[0] - bf16_low(w[x]), f[1] - bf16_high(w[x]));
                 }
             }
             const auto off = [r](int ch) { return (uint32_t)((ch >> 6) * C * 128 + sw_off(r, ch & 63)); };
             live = live && wait_warp(mi, B_FULL + st, g >> 1) && (g == 0 || wait_warp(mi, B_U, g - 1));
             if (n < C) {                       // tokens behind the end: whatever is there is no value
-                live = live && wait_warp(mi, B_FULLC + st, g >> 1);
                 if (live && r >= n) {
 #pragma unroll 1
                     for (int x = 0; x < DA / 2; x += 8) sts128(sb + off(half * (DA / 2) + x), 0, 0, 0, 0);
@@ -672,7 +744,6 @@ __device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Pa
             if (!live) continue;
             tc_fence_after();
             if (mine) {
-                const uint64_t minus = two(-1.f, -1.f);
 #pragma unroll 1
                 for (int rows = 0; rows < 32; rows += 16) {
                     const int ch = 32 * quad + rows + 8 * ((lane >> 3) & 1);
@@ -687,9 +758,9 @@ __device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Pa
                             ldmatrix_x4_trans(v, from + sw_off(tok, ch & 63));
 #pragma unroll
                             for (int y = 0; y < 4; ++y) {
-                                const uint64_t f = mul2(unpack2(v[y]), w[x + z + (y >> 1)]);
-                                hi[2 * z + y] = pack2(f);
-                                lo[2 * z + y] = pack2(fma2(unpack2(hi[2 * z + y]), minus, f));
+                                const uint32_t w1 = w[x + z + (y >> 1)], w2 = wlo[x + z + (y >> 1)], h = mul_bf16x2(v[y], w1);
+                                hi[2 * z + y] = h;
+                                lo[2 * z + y] = fma_bf16x2(v[y], w2, fma_bf16x2(v[y], w1, h ^ 0x80008000u));
                             }
                         }
                         tmem_st_16x128b_x4(tK + 4 * x + ((uint32_t)rows << 16), hi);
@@ -699,15 +770,13 @@ __device__ __forceinline__ void run_keys(unsigned char *smem, Misc &mi, const Pa
                 tc_wait_st();
             }
             tc_fence_before();
-            if (!(live = wait_warp(mi, B_FULLC + st, g >> 1))) continue;
             uint32_t odd = 0;
 #pragma unroll
             for (int x = 0; x < NC; x += 8) {
                 const uint4 v = lds128(sc + off(half * NC + x));
-                odd |= ((v.x & 0x7fff7fffu) + 0x00800080u) | ((v.y & 0x7fff7fffu) + 0x00800080u) | ((v.z & 0x7fff7fffu) + 0x00800080u) |
-                       ((v.w & 0x7fff7fffu) + 0x00800080u);
+                odd = max_abs_bf16x2(v.x, max_abs_bf16x2(v.y, max_abs_bf16x2(v.z, max_abs_bf16x2(v.w, odd))));
             }
-            if (odd & 0x80008000u) {
+            if (((odd & 0x7fff7fffu) + 0x00800080u) & 0x80008000u) {
 #pragma unroll 1
                 for (int x = half * NC; x < (half + 1) * NC; ++x) {
                     const uint32_t at = sc + off(x);
@@ -731,7 +800,7 @@ __global__ void __launch_bounds__(kThreads, 1) sfda_linear_tc_kernel(const __gri
     Misc &mi = *reinterpret_cast<Misc *>(smem + Layout<DA, DC>::kMisc);
     const int tid = threadIdx.x, warp = tid >> 5;
     if (tid == 0) {
-        const int counts[kBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 256, 1, 256, 1, 256, 256, 256, 256};
+        const int counts[kBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 256, 1, 256, 1, 256, 256, 256, 256};
         for (int i = 0; i < kBars; ++i) mbar_init(&mi.bars[i], counts[i]);
         mi.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -756,8 +825,8 @@ __global__ void __launch_bounds__(kThreads, 1) sfda_linear_tc_kernel(const __gri
     } else if (warp >= kWarpS) {
         regs_inc<kRegsS>();
         run_state<DA, DC, kStates>(smem, mi, p, tmem);
-    } else if (!kStates) {
-        run_p<DA, DC>(smem, mi, p, tmem);
+    } else {
+        if (!kStates) run_p<DA, DC>(smem, mi, p, tmem);
     }
     tc_fence_before();
     __syncthreads();
