@@ -79,7 +79,10 @@ def _bind_decode():
     with _LOCK:
         if _host is None:
             _host = _load_host()
-        _host.bind(ctypes.cast(lib.sfda_step, _vp).value, ctypes.cast(lib.sfda_step_fused, _vp).value)
+        address = lambda name: ctypes.cast(getattr(lib, name), _vp).value  # noqa: E731
+        _host.bind(address("sfda_step"), address("sfda_step_fused"))
+        _host.bind_operators(address("sfda_linear_step"), address("sfda_linear_forward"), address("sfda_linear_backward"),
+                             address("sfda_rotary"), address("sfda_group_norm"), address("sfda_group_norm_backward"))
         _BOUND = lib
 
 
@@ -544,52 +547,13 @@ SFDA_ROTARY_PLAIN, SFDA_ROTARY_LINEAR, SFDA_ROTARY_BASE, SFDA_ROTARY_PARTS = 0, 
 SFDA_ACT_NONE, SFDA_ACT_SILU = 0, 1
 
 
-def _take(t, name, dtype, shape, device, optional=False):
-    """A dense CUDA tensor of this type and shape on this device, which is the current one."""
-    if t is None:
-        if not optional:
-            raise TypeError(name + " must be a tensor")
-        return
-    _check(t, name, dtype)
-    if t.shape != shape:
-        raise ValueError("%s must be %s, not %s" % (name, list(shape), list(t.shape)))
-    if t.get_device() != device:
-        raise ValueError("%s must live on the same device as the first tensor" % name)
-
-
-def _current(t, name):
-    """The device of the call's first tensor: the current one, whose stream the work goes to."""
-    if not t.is_cuda:
-        raise ValueError(name + " must live on cuda")
-    device = t.get_device()
-    if device != torch._C._cuda_getDevice():
-        raise ValueError("%s must live on the current device" % name)
-    return device
-
-
-def _linear_shapes(q, k, v, log_decay, lens, S0, o, S_T):
-    """The checks that the forward and its gradients share: (B, T, H, H_kv, d_k, d_v), the type, the device."""
-    device = _current(q, "q")
-    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
-        raise ValueError("q must be [B, T, H, d_k], k [B, T, H_kv, d_k] and v [B, T, H_kv, d_v]")
-    B, T, H, d_k = q.shape
-    H_kv, d_v = v.shape[2:]
-    for t, n, shape in ((q, "q", (B, T, H, d_k)), (k, "k", (B, T, H_kv, d_k)), (v, "v", (B, T, H_kv, d_v)), (o, "o", (B, T, H, d_v))):
-        _take(t, n, q.dtype, shape, device)
-    _take(log_decay, "log_decay", torch.float32, (H,), device)
-    _take(lens, "lens", torch.int32, (B,), device, optional=True)
-    for t, n in ((S0, "S0"), (S_T, "S_T")):
-        _take(t, n, torch.float32, (B, H, d_k, d_v), device, optional=True)
-    return (B, T, H, H_kv, d_k, d_v), _dtype_code(q), device
-
-
-def _scratch(workspace, device):
-    if workspace is None:
-        return 0
-    _check(workspace, "workspace")
-    if workspace.get_device() != device:
-        raise ValueError("workspace must live on the same device as the first tensor")
-    return workspace.numel() * workspace.element_size()
+def _native(name, *args):
+    """A call through the extension, which checks types, shapes, layout and devices (all tensors on the current one)."""
+    if _BOUND is None or _BOUND is not _LIB:
+        _bind_decode()
+    rc = getattr(_host, name)(*args)
+    if rc != 0:
+        raise SfdaError(rc, "sfda_" + name)
 
 
 def sfda_linear_workspace_bytes(B, T, H, H_kv, d_k, d_v, dtype) -> int:
@@ -598,11 +562,7 @@ def sfda_linear_workspace_bytes(B, T, H, H_kv, d_k, d_v, dtype) -> int:
 
 def sfda_linear_forward(q, k, v, log_decay, lens, S0, o, S_T, scale=1.0, workspace=None, stream=None):
     """``sfda_linear_forward`` of ``include/sfda.h``: linear attention with a fixed decay for each head."""
-    sizes, code, device = _linear_shapes(q, k, v, log_decay, lens, S0, o, S_T)
-    rc = load().sfda_linear_forward(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lens), _ptr(S0), _ptr(o), _ptr(S_T), *sizes,
-                                    code, scale, _ptr(workspace), _scratch(workspace, device), _stream(stream))
-    if rc != 0:
-        raise SfdaError(rc, "sfda_linear_forward")
+    _native("linear_forward", q, k, v, log_decay, lens, S0, o, S_T, scale, workspace, stream)
 
 
 def sfda_linear_backward_workspace_bytes(B, T, H, H_kv, d_k, d_v, dtype) -> int:
@@ -611,53 +571,12 @@ def sfda_linear_backward_workspace_bytes(B, T, H, H_kv, d_k, d_v, dtype) -> int:
 
 def sfda_linear_backward(q, k, v, log_decay, lens, S0, d_o, dS_T, dq, dk, dv, dS0, scale=1.0, workspace=None, stream=None):
     """``sfda_linear_backward`` of ``include/sfda.h``: its gradients."""
-    sizes, code, device = _linear_shapes(q, k, v, log_decay, lens, S0, d_o, dS_T)
-    for t, n, like in ((dq, "dq", q), (dk, "dk", k), (dv, "dv", v)):
-        _take(t, n, q.dtype, like.shape, device)
-    _take(dS0, "dS0", torch.float32, (sizes[0], sizes[2], sizes[4], sizes[5]), device)
-    rc = load().sfda_linear_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lens), _ptr(S0), _ptr(d_o), _ptr(dS_T),
-                                     _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dS0), *sizes, code, scale, _ptr(workspace),
-                                     _scratch(workspace, device), _stream(stream))
-    if rc != 0:
-        raise SfdaError(rc, "sfda_linear_backward")
+    _native("linear_backward", q, k, v, log_decay, lens, S0, d_o, dS_T, dq, dk, dv, dS0, scale, workspace, stream)
 
 
 def sfda_linear_step(q, k, v, log_decay, S, o, scale=1.0, stream=None):
     """``sfda_linear_step`` of ``include/sfda.h``: one token of it; S is updated in place."""
-    device = _current(q, "q")
-    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
-        raise ValueError("q must be [B, H, d_k], k [B, H_kv, d_k] and v [B, H_kv, d_v]")
-    B, H, d_k = q.shape
-    H_kv, d_v = v.shape[1:]
-    for t, n, shape in ((q, "q", (B, H, d_k)), (k, "k", (B, H_kv, d_k)), (v, "v", (B, H_kv, d_v)), (o, "o", (B, H, d_v))):
-        _take(t, n, q.dtype, shape, device)
-    _take(log_decay, "log_decay", torch.float32, (H,), device)
-    _take(S, "S", torch.float32, (B, H, d_k, d_v), device)
-    rc = load().sfda_linear_step(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(S), _ptr(o), B, H, H_kv, d_k, d_v, _dtype_code(q),
-                                 scale, _stream(stream))
-    if rc != 0:
-        raise SfdaError(rc, "sfda_linear_step")
-
-
-def _rows(t, name, like, device):
-    """[..., heads, d] with dense heads and one stride from token to token: that stride in elements."""
-    if t.dim() != 4 and t.dim() != 3:
-        raise ValueError(name + " must be [B, T, heads, d] or [B, heads, d]")
-    if not t.is_cuda or t.get_device() != device:
-        raise ValueError("%s must live on the same device as the first tensor" % name)
-    if t.dtype is not like.dtype:
-        raise TypeError("%s must be %s" % (name, like.dtype))
-    if t.shape[:-2] != like.shape[:-2] or t.shape[-1] != like.shape[-1]:
-        raise ValueError("%s does not have the tokens and channels of the other tensors" % name)
-    d, h = t.shape[-1], t.shape[-2]
-    if (d > 1 and t.stride(-1) != 1) or (h > 1 and t.stride(-2) != d):
-        raise ValueError(name + " must have dense heads")
-    tokens = [(n, s) for n, s in zip(t.shape[:-2], t.stride()[:-2]) if n > 1]
-    if not tokens:
-        return h * d
-    if len(tokens) == 2 and tokens[0][1] != tokens[1][0] * tokens[1][1]:
-        raise ValueError(name + " must have one stride from token to token")
-    return tokens[-1][1]
+    _native("linear_step", q, k, v, log_decay, S, o, scale, stream)
 
 
 def sfda_rotary_turns(rot, base=10000.0, scaling=SFDA_ROTARY_PLAIN, factor=1.0, low=1.0, high=4.0, trained=8192.0):
@@ -674,48 +593,13 @@ def sfda_rotary(q, k, positions, turns, q_out, k_out, layout=SFDA_ROTARY_PAIRS, 
     """``sfda_rotary`` of ``include/sfda.h``: q [B, T, H, d] (or [B, H, d], one token each) and k, which may be None, turned by
     ``positions`` (int32, [B, T] or [B]); ``turns`` gives rot / 2 frequencies.  Slices of a packed projection are taken as they
     are; ``inverse`` turns gradients back."""
-    device = _current(q, "q")
-    strides = [_rows(q, "q", q, device), _rows(q_out, "q_out", q, device)]
-    if q_out.shape != q.shape:
-        raise ValueError("q_out must be %s, not %s" % (list(q.shape), list(q_out.shape)))
-    strides += [0, 0]
-    if (k is None) != (k_out is None):
-        raise TypeError("k and k_out go together")
-    if k is not None:
-        strides[2:] = [_rows(k, "k", q, device), _rows(k_out, "k_out", q, device)]
-        if k_out.shape != k.shape:
-            raise ValueError("k_out must be %s, not %s" % (list(k.shape), list(k_out.shape)))
-    B, T = (q.shape[0], q.shape[1]) if q.dim() == 4 else (q.shape[0], 1)
-    _take(positions, "positions", torch.int32, (B, T) if q.dim() == 4 or positions.dim() == 2 else (B,), device)
-    _take(turns, "turns", torch.int64, (turns.numel(),), device)
-    rc = load().sfda_rotary(_ptr(q), _ptr(k), _ptr(positions), _ptr(turns), _ptr(q_out), _ptr(k_out), B, T, q.shape[-2],
-                            0 if k is None else k.shape[-2], q.shape[-1], 2 * turns.numel(), strides[0], strides[2], strides[1],
-                            strides[3], layout, amplitude, int(inverse), _dtype_code(q), _stream(stream))
-    if rc != 0:
-        raise SfdaError(rc, "sfda_rotary")
-
-
-def _norm_shapes(x, weight, bias, gate, others):
-    device = _current(x, "x")
-    if x.dim() < 1 or x.numel() == 0:
-        raise ValueError("x must be [..., C] with at least one row")
-    C = x.shape[-1]
-    for t, n in ((x, "x"),) + others:
-        _take(t, n, x.dtype, x.shape, device)
-    _take(gate, "gate", x.dtype, x.shape, device, optional=True)
-    for t, n in ((weight, "weight"), (bias, "bias")):
-        _take(t, n, torch.float32, (C,), device, optional=True)
-    return x.numel() // C, C, _dtype_code(x), device
+    _native("rotary", q, k, positions, turns, q_out, k_out, layout, amplitude, inverse, stream)
 
 
 def sfda_group_norm(x, weight, bias, gate, y, groups, eps=1e-5, act=SFDA_ACT_NONE, stream=None):
     """``sfda_group_norm`` of ``include/sfda.h``: x [..., C] normalised over each of ``groups`` groups of channels; weight, bias
     and gate may be None."""
-    rows, C, code, _ = _norm_shapes(x, weight, bias, gate, ((y, "y"),))
-    rc = load().sfda_group_norm(_ptr(x), _ptr(weight), _ptr(bias), _ptr(gate), _ptr(y), rows, C, groups, eps, act, code,
-                                _stream(stream))
-    if rc != 0:
-        raise SfdaError(rc, "sfda_group_norm")
+    _native("group_norm", x, weight, bias, gate, y, groups, eps, act, stream)
 
 
 def sfda_group_norm_backward_workspace_bytes(rows, C) -> int:
@@ -725,12 +609,4 @@ def sfda_group_norm_backward_workspace_bytes(rows, C) -> int:
 def sfda_group_norm_backward(x, weight, bias, gate, dy, dx, dweight, dbias, dgate, groups, eps=1e-5, act=SFDA_ACT_NONE,
                              workspace=None, stream=None):
     """``sfda_group_norm_backward`` of ``include/sfda.h``; dweight and dbias may be None, dgate is None without a gate."""
-    rows, C, code, device = _norm_shapes(x, weight, bias, gate, ((dy, "dy"), (dx, "dx")))
-    for t, n in ((dweight, "dweight"), (dbias, "dbias")):
-        _take(t, n, torch.float32, (C,), device, optional=True)
-    _take(dgate, "dgate", x.dtype, x.shape, device, optional=gate is None)
-    rc = load().sfda_group_norm_backward(_ptr(x), _ptr(weight), _ptr(bias), _ptr(gate), _ptr(dy), _ptr(dx), _ptr(dweight),
-                                         _ptr(dbias), _ptr(dgate), rows, C, groups, eps, act, code, _ptr(workspace),
-                                         _scratch(workspace, device), _stream(stream))
-    if rc != 0:
-        raise SfdaError(rc, "sfda_group_norm_backward")
+    _native("group_norm_backward", x, weight, bias, gate, dy, dx, dweight, dbias, dgate, groups, eps, act, workspace, stream)

@@ -84,8 +84,9 @@ def host_hash() -> str:
 
     import torch
     h = hashlib.sha256(" ".join(_host_command("") + [torch.__version__, sys.version, str(sysconfig.get_config_var("SOABI"))]).encode())
-    with open(os.path.join(CSRC, "sfda_host.cpp"), "rb") as f:
-        h.update(f.read())
+    for path in (os.path.join(CSRC, "sfda_host.cpp"), os.path.join(HERE, "..", "include", "sfda.h")):
+        with open(path, "rb") as f:
+            h.update(f.read())
     return h.hexdigest()
 
 

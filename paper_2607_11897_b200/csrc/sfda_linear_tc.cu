@@ -903,22 +903,25 @@ cudaError_t launch_one(Params &p, cudaStream_t stream, int *launches)
 
 }  // namespace
 
-// How many stretches each sequence is cut into, for `chains` of `chunks` chunks on n SMs.  In units of a chunk's share of the
-// memory's time on n SMs: a CTA alone needs at least kAlone of it; a cut costs a pass over b and c, and a unit its start.
+// How many stretches each sequence is cut into, for `chains` of `chunks` chunks on n SMs: the least of a sum of measured times in
+// microseconds.  A CTA takes kChunk for a chunk (kStates for one of the pass that only makes states) and kStart for a unit; a
+// stretch reads the states of those before it, kCarry each; a second launch costs kLaunch; and memory takes kMemory for a chunk.
+// (Measured: one sequence of 131072 tokens and 16 heads 2850 us uncut, 720 in 8; 4 x 4096 and 16 heads 115 uncut, 108 in 2; 1024
+// and 8 heads 32 uncut, 39 in 2.)
 static int stretches(long long chains, int chunks, int n)
 {
-    constexpr double kAlone = 0.6, kStart = 1.0, kLaunch = 1.5;
+    constexpr double kChunk = 2.9, kStates = 2.6, kStart = 8.0, kCarry = 2.5, kLaunch = 4.0, kMemory = 0.026;
     const auto waves = [n](long long units) { return (double)((units + n - 1) / n); };
     int best = 1;
     double least = 0;
     for (int s = 1; s <= chunks && s <= 64; ++s) {
         const int cps = (chunks + s - 1) / s;
         if ((chunks + cps - 1) / cps != s) continue;
-        double t = waves(chains * s) * (cps * kAlone + kStart);
-        const double mem = (double)chains * chunks / n;
+        const double mem = (double)chains * chunks * kMemory;
+        double t = waves(chains * s) * (cps * kChunk + kStart + (s - 1) * kCarry);
         if (t < mem) t = mem;
         if (s > 1) {
-            double a = waves(chains * (s - 1)) * (cps * 0.5 * kAlone + kStart);
+            double a = waves(chains * (s - 1)) * (cps * kStates + kStart);
             if (a < 0.5 * mem) a = 0.5 * mem;
             t += a + kLaunch;
         }
