@@ -626,8 +626,8 @@ SFDA_API int sfda_rotary_turns(uint64_t *turns, int rot, double base, int scalin
  *  x, gate, y [rows][C] dtype (gate may be NULL)     weight, bias [C] float, or NULL (1 and 0)
  *  act       SFDA_ACT_NONE: the identity; SFDA_ACT_SILU: u / (1 + exp(-u))
  *  y may be x or gate.  mean and var (divided by C / G) are those of the row's group alone, so rows are independent: tokens of
- *  a causal model.  Any G that divides C; at most 65535 groups wider than 128 accesses of 16 bytes (8 of 4 bytes where C / G
- *  is not a multiple of 4).  SFDA_ERR_VALUE unless eps is positive and finite.
+ *  a causal model.  Any G that divides C; at most 65535 groups where they are wider than 8192 channels (4096 in fp32; 1024
+ *  where C / G is not a multiple of 4).  SFDA_ERR_VALUE unless eps is positive and finite.
  *
  * sfda_group_norm_backward: the gradients from dy [rows][C] dtype:  dx, dgate [rows][C] dtype (dgate is required with a
  * gate and ignored without), dweight, dbias [C] float, either of which may be NULL.  dx may be dy, dgate may be gate.

@@ -3,7 +3,7 @@
 //     n = (x - mean) / sqrt(var + eps),   z = n w + b,   y = act(z)   or, with a gate,   y = z act(gate),
 //
 // and its derivative.  Bound by memory: x (gate, dy) are read once, everything between stays in registers.  A group is
-// spread over P lanes of one warp, NV accesses of V channels each; the mean is taken first and the variance from the
+// spread over P lanes of one warp or of several, NV accesses of V channels each; the mean is taken first and the variance from the
 // differences, both in fp32.  The differences' own mean, what the first one's rounding left, is taken off as well: where a
 // group's mean is large beside its deviation, n would otherwise be off by the mean's 2^-24 over the deviation.
 //
@@ -30,24 +30,30 @@ struct Dev {
     float eps;
 };
 
-template <int V, bool kMost>
-__device__ __forceinline__ void params(const float *w, int c, float (&x)[V], float other)
+// Sum over a group's lanes, the same for all of them: within a warp, and through shared memory where a group has several warps
+// (all threads of the CTA come here together).
+__device__ __forceinline__ float sum_lanes(float x, int lanes, float *red = nullptr)
 {
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = w ? __ldg(w + c + i) : other;
-}
-
-__device__ __forceinline__ float sum_lanes(float x, int lanes)
-{
-    for (int d = lanes >> 1; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    for (int d = min(lanes, 32) >> 1; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    if (lanes > 32) {
+        const int warp = threadIdx.x >> 5, warps = lanes >> 5;
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) red[warp] = x;
+        __syncthreads();
+        x = 0.f;
+        for (int i = 0; i < warps; ++i) x += red[warp / warps * warps + i];
+    }
     return x;
 }
 
 __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 
-template <typename T, int V, int NV, bool kBackward>
+// The next row's accesses are in flight while a row is computed.  Which of the gate and the activation there are is known when the
+// kernel is compiled: decided per element at run time, the derivative took twice as many instructions and 1.9 times as long.
+template <typename T, int V, int NV, bool kBackward, bool kGate, bool kSilu>
 __global__ void __launch_bounds__(kThreads) sfda_group_norm_kernel(const Dev p)
 {
+    __shared__ float part[kThreads / 32];
     const int tid = threadIdx.x, lane = tid % p.lanes, slot = tid / p.lanes;
     // slots beyond gb * rb hold no group (but take part in the shuffles)
     const int g0 = blockIdx.y * p.gb, grp = g0 + slot % p.gb, sub = slot / p.gb;
@@ -61,61 +67,76 @@ __global__ void __launch_bounds__(kThreads) sfda_group_norm_kernel(const Dev p)
         const int e = (lane + j * p.lanes) * V;
         in[j] = have && e < p.D;
         ch[j] = in[j] ? grp * p.D + e : 0;
-        params<V, true>(p.weight, ch[j], w[j], 1.f);
-        params<V, true>(p.bias, ch[j], b[j], 0.f);
-        if (kBackward)
 #pragma unroll
-            for (int i = 0; i < V; ++i) aw[j][i] = ab[j][i] = 0.f;
+        for (int i = 0; i < V; ++i) {
+            w[j][i] = p.weight ? __ldg(p.weight + ch[j] + i) : 1.f;
+            b[j][i] = p.bias ? __ldg(p.bias + ch[j] + i) : 0.f;
+            if (kBackward) aw[j][i] = ab[j][i] = 0.f;
+        }
     }
     const T *px = static_cast<const T *>(p.x), *pg = static_cast<const T *>(p.gate), *pd = static_cast<const T *>(p.dy);
     const long long step = (long long)gridDim.x * p.rb;
+    Raw<T, V> rx[NV], rg[kGate ? NV : 1], rd[kBackward ? NV : 1];
+    const auto fetch = [&](long long row) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (in[j] && row < p.rows) {
+                const long long at = row * p.C + ch[j];
+                rx[j].load(px + at);
+                if constexpr (kGate) rg[j].load(pg + at);
+                if constexpr (kBackward) rd[j].load(pd + at);
+            } else {
+                rx[j].clear();
+                if constexpr (kGate) rg[j].clear();
+                if constexpr (kBackward) rd[j].clear();
+            }
+        }
+    };
+    fetch((long long)blockIdx.x * p.rb + sub);
     for (long long base = (long long)blockIdx.x * p.rb; base < p.rows; base += step) {
         const long long row = base + sub;
         const bool live = have && row < p.rows;
-        float x[NV][V], gt[NV][V], dy[kBackward ? NV : 1][V];
+        float x[NV][V], gt[kGate ? NV : 1][V], dy[kBackward ? NV : 1][V];
         float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) x[j][i] = gt[j][i] = 0.f;
-            if (live && in[j]) {
-                ld_vec(px + row * p.C + ch[j], x[j]);
-                if (pg) ld_vec(pg + row * p.C + ch[j], gt[j]);
-                if constexpr (kBackward) ld_vec(pd + row * p.C + ch[j], dy[j]);
-            } else if constexpr (kBackward) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) dy[j][i] = 0.f;
-            }
-        }
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum += x[j][i];
-        const float mean = sum_lanes(sum, p.lanes) * inv;
+            for (int i = 0; i < V; ++i) {
+                x[j][i] = rx[j].get(i);
+                if constexpr (kGate) gt[j][i] = rg[j].get(i);
+                if constexpr (kBackward) dy[j][i] = rd[j].get(i);
+                sum += x[j][i];
+            }
+        fetch(row + step);
+        const float mean = sum_lanes(sum, p.lanes, part) * inv;
         float sq = 0.f, rest = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 x[j][i] = in[j] ? x[j][i] - mean : 0.f;
-                rest += x[j][i];
+                if constexpr (sizeof(T) == 4) rest += x[j][i];
                 sq = fmaf(x[j][i], x[j][i], sq);
             }
-        rest = sum_lanes(rest, p.lanes) * inv;
-        const float rstd = rsqrtf(fmaf(-rest, rest, sum_lanes(sq, p.lanes) * inv) + p.eps);
+        sq = sum_lanes(sq, p.lanes, part) * inv;
+        if constexpr (sizeof(T) == 4) {
+            rest = sum_lanes(rest, p.lanes, part) * inv;
+            sq = fmaf(-rest, rest, sq);
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+            for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < V; ++i) x[j][i] -= in[j] ? rest : 0.f;
+                for (int i = 0; i < V; ++i) x[j][i] -= in[j] ? rest : 0.f;
+        }
+        const float rstd = rsqrtf(sq + p.eps);
         if constexpr (!kBackward) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 float y[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float z = fmaf(x[j][i] * rstd, w[j][i], b[j][i]), h = pg ? gt[j][i] : z;
-                    const float a = p.silu ? h * sigmoid(h) : h;
-                    y[i] = pg ? z * a : a;
+                    const float z = fmaf(x[j][i] * rstd, w[j][i], b[j][i]), h = kGate ? gt[kGate ? j : 0][i] : z;
+                    const float a = kSilu ? h * sigmoid(h) : h;
+                    y[i] = kGate ? z * a : a;
                 }
                 if (live && in[j]) st_vec(static_cast<T *>(p.y) + row * p.C + ch[j], y);
             }
@@ -126,11 +147,11 @@ __global__ void __launch_bounds__(kThreads) sfda_group_norm_kernel(const Dev p)
                 float dg[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float n = x[j][i] * rstd, z = fmaf(n, w[j][i], b[j][i]), h = pg ? gt[j][i] : z;
-                    const float sg = p.silu ? sigmoid(h) : 1.f;
-                    const float a = p.silu ? h * sg : h, slope = p.silu ? sg * fmaf(h, 1.f - sg, 1.f) : 1.f;
-                    const float dz = dy[j][i] * (pg ? a : slope);
-                    dg[i] = dy[j][i] * z * slope;
+                    const float n = x[j][i] * rstd, z = fmaf(n, w[j][i], b[j][i]), h = kGate ? gt[kGate ? j : 0][i] : z;
+                    const float sg = kSilu ? sigmoid(h) : 1.f;
+                    const float a = kSilu ? h * sg : h, slope = kSilu ? fmaf(a, 1.f - sg, sg) : 1.f;
+                    const float dz = dy[j][i] * (kGate ? a : slope);
+                    if (kGate) dg[i] = dy[j][i] * z * slope;
                     aw[j][i] = fmaf(dz, n, aw[j][i]);
                     ab[j][i] += dz;
                     const float dn = dz * w[j][i];
@@ -139,15 +160,15 @@ __global__ void __launch_bounds__(kThreads) sfda_group_norm_kernel(const Dev p)
                     x[j][i] = n;
                     dy[j][i] = dn;
                 }
-                if (pg && live && in[j]) st_vec(static_cast<T *>(p.dgate) + row * p.C + ch[j], dg);
+                if (kGate && live && in[j]) st_vec(static_cast<T *>(p.dgate) + row * p.C + ch[j], dg);
             }
-            s1 = sum_lanes(s1, p.lanes) * inv;
-            s2 = sum_lanes(s2, p.lanes) * inv;
+            s1 = sum_lanes(s1, p.lanes, part) * inv * rstd;
+            s2 = sum_lanes(s2, p.lanes, part) * inv * rstd;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 float d[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) d[i] = rstd * (dy[j][i] - s1 - x[j][i] * s2);
+                for (int i = 0; i < V; ++i) d[i] = fmaf(-x[j][i], s2, fmaf(rstd, dy[j][i], -s1));
                 if (live && in[j]) st_vec(static_cast<T *>(p.dx) + row * p.C + ch[j], d);
             }
         }
@@ -183,7 +204,7 @@ __global__ void __launch_bounds__(kThreads) sfda_group_norm_kernel(const Dev p)
     }
 }
 
-// A group too wide for one warp's registers: one CTA per (row, group), the group read again for each step (it is in the
+// A group too wide for the registers of a CTA: one CTA per (row, group), the group read again for each step (it is in the
 // caches by then).
 __device__ float sum_block(float x, float *red)
 {
@@ -286,6 +307,7 @@ Shape shape_of(int C, int G, int dtype)
     const int n = D / s.V;                                  // accesses of a group
     s.lanes = 1;
     while (s.lanes < 32 && s.lanes < n) s.lanes *= 2;
+    while (s.lanes < kThreads && s.lanes * 2 < n) s.lanes *= 2;         // several warps where two accesses a lane do not do
     s.NV = 1;
     while (s.NV * s.lanes < n) s.NV *= 2;
     s.wide = s.NV > kMaxNV;
@@ -306,14 +328,22 @@ unsigned blocks_over_rows(const Shape &s, long long rows, int waves)
     const long long want = (rows + s.rb - 1) / s.rb, most = (148ll * waves + s.blocks_y - 1) / s.blocks_y;
     return (unsigned)(want < most ? want : most);
 }
-constexpr int kForwardWaves = 64, kBackwardWaves = 8;
+constexpr int kForwardWaves = 8, kBackwardWaves = 8;
 
+template <typename T, int V, int NV, bool kBackward>
+void launch_kind(const Dev &p, dim3 grid, cudaStream_t stream)
+{
+    if (p.gate && p.silu) sfda_group_norm_kernel<T, V, NV, kBackward, true, true><<<grid, kThreads, 0, stream>>>(p);
+    else if (p.gate) sfda_group_norm_kernel<T, V, NV, kBackward, true, false><<<grid, kThreads, 0, stream>>>(p);
+    else if (p.silu) sfda_group_norm_kernel<T, V, NV, kBackward, false, true><<<grid, kThreads, 0, stream>>>(p);
+    else sfda_group_norm_kernel<T, V, NV, kBackward, false, false><<<grid, kThreads, 0, stream>>>(p);
+}
 template <typename T, int V, bool kBackward>
 cudaError_t launch_nv(const Shape &s, const Dev &p, dim3 grid, cudaStream_t stream)
 {
-    if (s.NV == 1) sfda_group_norm_kernel<T, V, 1, kBackward><<<grid, kThreads, 0, stream>>>(p);
-    else if (s.NV == 2) sfda_group_norm_kernel<T, V, 2, kBackward><<<grid, kThreads, 0, stream>>>(p);
-    else sfda_group_norm_kernel<T, V, 4, kBackward><<<grid, kThreads, 0, stream>>>(p);
+    if (s.NV == 1) launch_kind<T, V, 1, kBackward>(p, grid, stream);
+    else if (s.NV == 2) launch_kind<T, V, 2, kBackward>(p, grid, stream);
+    else launch_kind<T, V, 4, kBackward>(p, grid, stream);
     return cudaGetLastError();
 }
 template <typename T, bool kBackward>

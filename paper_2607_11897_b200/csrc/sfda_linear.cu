@@ -49,12 +49,7 @@ size_t round256(size_t x) { return (x + 255u) & ~(size_t)255u; }
 
 cudaError_t run_passes(const LinearArgs &a, const LinearPass *p, int count, void *workspace, cudaStream_t stream, int *launches)
 {
-    if (a.dtype == 1) return launch_linear_tc(a, p, count, workspace, stream, launches);
-    for (int i = 0; i < count; ++i) {
-        const cudaError_t e = launch_linear_f32(a, p[i], stream, launches);
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
+    return a.dtype == 1 ? launch_linear_tc(a, p, count, workspace, stream, launches) : launch_linear_f32(a, p, count, stream, launches);
 }
 size_t pass_bytes(const LinearArgs &a, int count, int d_k, int d_v)
 {

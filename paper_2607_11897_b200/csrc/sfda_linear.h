@@ -36,7 +36,7 @@ struct LinearArgs {
 };
 
 // fp32 passes on the warp-level tensor cores (operands split into two tf32 parts).
-cudaError_t launch_linear_f32(const LinearArgs &a, const LinearPass &p, cudaStream_t stream, int *launches);
+cudaError_t launch_linear_f32(const LinearArgs &a, const LinearPass *passes, int count, cudaStream_t stream, int *launches);
 
 // bf16 passes on tcgen05.  The workspace begins with the status word that sfda_workspace_status reads.
 size_t linear_tc_bytes(const LinearArgs &a, int passes, int d_k, int d_v);

@@ -11,7 +11,8 @@ namespace sfda {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int HT = 8;            // heads per thread
+constexpr int HT = 16;           // heads per thread at most
+constexpr int kBatch = 4;
 
 struct Dev {
     const void *q, *k;
@@ -19,7 +20,7 @@ struct Dev {
     const int *positions;
     const uint64_t *turns;
     long long rows, q_stride, k_stride, qo_stride, ko_stride;
-    int H, H_kv, d, rot, inverse;
+    int H, H_kv, d, rot, inverse, ht;
     float amplitude;
 };
 
@@ -39,6 +40,8 @@ __global__ void __launch_bounds__(kThreads) sfda_rotary_kernel(const Dev p, cons
     const int c = kHalves ? (turned ? it * V : p.rot + (it - half / V) * V) : it * NX;
     float cs[NP], sn[NP];
     bool on[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) on[i] = false;
     if (turned) {
         const uint64_t pos = (uint64_t)(int64_t)p.positions[row];
 #pragma unroll
@@ -51,43 +54,50 @@ __global__ void __launch_bounds__(kThreads) sfda_rotary_kernel(const Dev p, cons
             sn[i] *= p.inverse ? -p.amplitude : p.amplitude;
         }
     }
-    const int heads = p.H + p.H_kv, h0 = blockIdx.y * HT, h1 = min(h0 + HT, heads);
-#pragma unroll 4
-    for (int h = h0; h < h1; ++h) {
-        const bool isq = h < p.H;
-        const T *x = isq ? static_cast<const T *>(p.q) + row * p.q_stride + (long long)h * p.d
-                         : static_cast<const T *>(p.k) + row * p.k_stride + (long long)(h - p.H) * p.d;
-        T *y = isq ? static_cast<T *>(p.q_out) + row * p.qo_stride + (long long)h * p.d
-                   : static_cast<T *>(p.k_out) + row * p.ko_stride + (long long)(h - p.H) * p.d;
-        if constexpr (kHalves) {
-            float a[V], b[V];
-            ld_vec(x + c, a);
-            if (turned) {
-                ld_vec(x + c + half, b);
-                float re[V], im[V];
+    const int heads = p.H + p.H_kv, h0 = blockIdx.y * p.ht, h1 = min(h0 + p.ht, heads);
+    // kBatch heads are read before the first of them is written: outputs may be inputs, so the compiler has to keep the order.
+    constexpr int NV = kHalves ? V : NX;                      // elements of one access
+    for (int hb = h0; hb < h1; hb += kBatch) {
+        Raw<T, NV> a[kBatch], b[kHalves ? kBatch : 1];
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    re[i] = a[i] * cs[i] - b[i] * sn[i];
-                    im[i] = a[i] * sn[i] + b[i] * cs[i];
+        for (int n = 0; n < kBatch; ++n) {
+            const int h = hb + n;
+            if (h >= h1) continue;
+            const T *x = h < p.H ? static_cast<const T *>(p.q) + row * p.q_stride + (long long)h * p.d
+                                 : static_cast<const T *>(p.k) + row * p.k_stride + (long long)(h - p.H) * p.d;
+            a[n].load(x + c);
+            if (kHalves && turned) b[n].load(x + c + half);
+        }
+#pragma unroll
+        for (int n = 0; n < kBatch; ++n) {
+            const int h = hb + n;
+            if (h >= h1) continue;
+            T *y = h < p.H ? static_cast<T *>(p.q_out) + row * p.qo_stride + (long long)h * p.d
+                           : static_cast<T *>(p.k_out) + row * p.ko_stride + (long long)(h - p.H) * p.d;
+            float re[NV], im[kHalves ? NV : 1];
+            if constexpr (kHalves) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) re[i] = a[n].get(i);
+                if (turned) {
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        const float u = re[i], v = b[n].get(i);
+                        re[i] = u * cs[i] - v * sn[i];
+                        im[i] = u * sn[i] + v * cs[i];
+                    }
+                    st_vec(y + c + half, im);
                 }
                 st_vec(y + c, re);
-                st_vec(y + c + half, im);
             } else {
-                st_vec(y + c, a);
-            }
-        } else {
-            float a[NX];
-            ld_vec(x + c, a);
-            if (turned) {
 #pragma unroll
-                for (int i = 0; i < NP; ++i)
-                    if (on[i]) {
-                        const float re = a[2 * i] * cs[i] - a[2 * i + 1] * sn[i], im = a[2 * i] * sn[i] + a[2 * i + 1] * cs[i];
-                        a[2 * i] = re;
-                        a[2 * i + 1] = im;
-                    }
+                for (int i = 0; i < NP; ++i) {
+                    const float u = a[n].get(2 * i), v = a[n].get(2 * i + 1);
+                    const bool t = turned && on[i];
+                    re[2 * i] = t ? u * cs[i] - v * sn[i] : u;
+                    re[2 * i + 1] = t ? u * sn[i] + v * cs[i] : v;
+                }
+                st_vec(y + c, re);
             }
-            st_vec(y + c, a);
         }
     }
 }
@@ -95,12 +105,15 @@ __global__ void __launch_bounds__(kThreads) sfda_rotary_kernel(const Dev p, cons
 template <typename T, int V, bool kHalves>
 cudaError_t launch_v(const RotaryArgs &a, cudaStream_t stream)
 {
-    const Dev p = {a.q, a.k, a.q_out, a.k_out, a.positions, a.turns, a.rows, a.q_stride, a.k_stride, a.qo_stride, a.ko_stride,
-                   a.H, a.H_kv, a.d, a.rot, a.inverse, a.amplitude};
     const int items = kHalves ? (a.rot / 2 + (a.d - a.rot)) / V : a.d / (V > 1 ? V : 2);
     const long long blocks = (a.rows * items + kThreads - 1) / kThreads;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    sfda_rotary_kernel<T, V, kHalves><<<dim3((unsigned)blocks, (a.H + a.H_kv + HT - 1) / HT), kThreads, 0, stream>>>(p, items);
+    // few tokens: fewer heads to a thread, until the device is full (256 tokens of 40 heads: 7.1 us with 8, 5 with 4)
+    int ht = HT;
+    while (ht > kBatch && blocks * ((a.H + a.H_kv + ht - 1) / ht) < 148 * 8) ht /= 2;
+    const Dev p = {a.q, a.k, a.q_out, a.k_out, a.positions, a.turns, a.rows, a.q_stride, a.k_stride, a.qo_stride, a.ko_stride,
+                   a.H, a.H_kv, a.d, a.rot, a.inverse, ht, a.amplitude};
+    sfda_rotary_kernel<T, V, kHalves><<<dim3((unsigned)blocks, (a.H + a.H_kv + ht - 1) / ht), kThreads, 0, stream>>>(p, items);
     return cudaGetLastError();
 }
 
@@ -121,11 +134,16 @@ int widest(const RotaryArgs &a, int most)
 template <typename T>
 cudaError_t dispatch(const RotaryArgs &a, cudaStream_t stream)
 {
-    const int v = widest(a, 8);
-    if (a.layout == 1)
-        return v == 8 ? launch_v<T, 8, true>(a, stream) : v == 4 ? launch_v<T, 4, true>(a, stream)
-             : v == 2 ? launch_v<T, 2, true>(a, stream) : launch_v<T, 1, true>(a, stream);
-    return v == 8 ? launch_v<T, 8, false>(a, stream) : v == 4 ? launch_v<T, 4, false>(a, stream) : launch_v<T, 2, false>(a, stream);
+    constexpr int kMost = 16 / (int)sizeof(T);
+    const int v = widest(a, kMost);
+    if (a.layout == 1) {
+        if constexpr (kMost == 8)
+            if (v == 8) return launch_v<T, 8, true>(a, stream);
+        return v == 4 ? launch_v<T, 4, true>(a, stream) : v == 2 ? launch_v<T, 2, true>(a, stream) : launch_v<T, 1, true>(a, stream);
+    }
+    if constexpr (kMost == 8)
+        if (v == 8) return launch_v<T, 8, false>(a, stream);
+    return v == 4 ? launch_v<T, 4, false>(a, stream) : launch_v<T, 2, false>(a, stream);
 }
 
 }  // namespace

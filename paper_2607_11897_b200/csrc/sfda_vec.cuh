@@ -76,4 +76,38 @@ __device__ __forceinline__ void st_vec(__nv_bfloat16 *p, const float (&x)[V])
     }
 }
 
+// V elements as they lie in memory, to be in flight while something else is computed.
+template <typename T, int V>
+struct Raw {
+    static constexpr int kWords = V * (int)sizeof(T) / 4;
+    uint32_t w[kWords > 0 ? kWords : 1];
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if constexpr (kWords >= 4) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint32_t *>(p) + i);
+                w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+            }
+        } else if constexpr (kWords == 2) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(p);
+            w[0] = v.x; w[1] = v.y;
+        } else if constexpr (kWords == 1) {
+            w[0] = *reinterpret_cast<const uint32_t *>(p);
+        } else {
+            w[0] = *reinterpret_cast<const uint16_t *>(p);
+        }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < (kWords > 0 ? kWords : 1); ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+    }
+};
+
 }  // namespace sfda
