@@ -28,6 +28,12 @@ __device__ __forceinline__ void split_tf32(float x, uint32_t &hi, uint32_t &lo)
     hi = __float_as_uint(x) & 0xffffe000u;                 // the tensor core reads 10 mantissa bits: cut, not rounded,
     lo = __float_as_uint(x - __uint_as_float(hi));         // so that the rest is exact
 }
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2])
+{
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
 // c += A B for one 16 x 8 tile and 8 values of k, both operands in two parts.  The tensor core cuts its sums off instead of
 // rounding them, always towards zero: the small products are summed by themselves, and no sum runs for longer than one
 // product of a chunk before fp32 additions take it over (a state of 3000 tokens summed in its accumulators was 9e-6 off).
@@ -38,9 +44,9 @@ __device__ __forceinline__ void mma3(float (&c)[4], float (&c_lo)[4], const floa
     for (int i = 0; i < 4; ++i) split_tf32(a[i], ah[i], al[i]);
 #pragma unroll
     for (int i = 0; i < 2; ++i) split_tf32(b[i], bh[i], bl[i]);
-    tc::mma_tf32(c_lo, al, bh);
-    tc::mma_tf32(c_lo, ah, bl);
-    tc::mma_tf32(c, ah, bh);
+    mma(c_lo, al, bh);
+    mma(c, ah, bh);
+    mma(c_lo, ah, bl);
 }
 
 struct Pass {
@@ -63,6 +69,7 @@ struct Smem {
     static constexpr int LA = DA + 4, LC = CB + 8, LP = L + 4;
     float a[2][L * LA], b[2][L * LA], c[2][L * LC], S[DA * LC], P[L * LP];
     float pw[L + 4];             // g^0 .. g^64
+    float w[2][L];               // the chunk's weights of b; of two chunks, for one is written while the other is read
     int first[CB];               // first token (in the pass's order) whose value of this column was not finite
 };
 
@@ -127,9 +134,18 @@ __global__ void __launch_bounds__(kThreads) sfda_linear_f32_kernel(const Dev dev
     keep_copy();
     __syncthreads();
 
+    int decay_of = 0;                                          // the chunk length that gm is for
+    float gm = 0.f;
+    bool weak = false;
     for (int ci = 0; ci < chunks; ++ci) {
         const int t0 = (rev ? chunks - 1 - ci : ci) * L, n = min(L, len - t0), buf = ci & 1;
         float *sa = s.a[buf], *sb = s.b[buf], *sc = s.c[buf];
+        if (n != decay_of) {
+            decay_of = n;
+            weak = (float)n * ld > -0.5f;
+            gm = weak ? expm1f((float)n * ld) : expf((float)n * ld);
+        }
+        if (tid < L) s.w[buf][tid] = tid < n ? p.sw * s.pw[rev ? tid + 1 : n - 1 - tid] : 0.f;
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         for (int x = tid; x < L * CB / 4; x += kThreads) {     // the thread's own copies
             const int r = x / (CB / 4), d = x % (CB / 4) * 4;
@@ -143,10 +159,9 @@ __global__ void __launch_bounds__(kThreads) sfda_linear_f32_kernel(const Dev dev
         __syncthreads();                                       // the tiles, the state's copy; the other tiles' readers are done
         if (ci + 1 < chunks) fetch(ci + 1);
 
-        {   // P = (a b^T) o D: the warp's 16 rows and 32 columns, the tiles of 8 columns that the mask leaves
+        {   // P = (a b^T) o D: the warp's 16 rows and 32 columns, unless the mask leaves none of them
             const int r0 = 16 * (warp & 3), q0 = 32 * (warp >> 2);
-            const int j0 = rev ? max(0, (r0 - q0) / 8) : 0, j1 = rev ? 4 : min(4, (r0 + 16 - q0 + 7) / 8);
-            if (j0 < j1) {
+            if (rev ? q0 + 31 >= r0 : q0 <= r0 + 15) {
                 float acc[4][4] = {}, low[4][4] = {};
 #pragma unroll 2
                 for (int k0 = 0; k0 < DA; k0 += 8) {
@@ -154,20 +169,23 @@ __global__ void __launch_bounds__(kThreads) sfda_linear_f32_kernel(const Dev dev
 #pragma unroll
                     for (int x = 0; x < 4; ++x) av[x] = sa[(r0 + g + 8 * (x & 1)) * Sm::LA + k0 + tg + 4 * (x >> 1)];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (j >= j0 && j < j1) {
-                            float bv[2] = {sb[(q0 + 8 * j + g) * Sm::LA + k0 + tg], sb[(q0 + 8 * j + g) * Sm::LA + k0 + tg + 4]};
-                            mma3(acc[j], low[j], av, bv);
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        float bv[2] = {sb[(q0 + 8 * j + g) * Sm::LA + k0 + tg], sb[(q0 + 8 * j + g) * Sm::LA + k0 + tg + 4]};
+                        mma3(acc[j], low[j], av, bv);
+                    }
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j >= j0 && j < j1)
+                for (int j = 0; j < 4; ++j) {
+                    float f[4];                                // every power is read before the mask applies: no branches
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int t = r0 + g + 8 * (x >> 1), i = q0 + 8 * j + 2 * tg + (x & 1), gap = rev ? i - t : t - i;
-                            s.P[t * Sm::LP + i] = gap >= 0 ? (acc[j][x] + low[j][x]) * (p.sp * s.pw[gap]) : 0.f;
-                        }
+                    for (int x = 0; x < 4; ++x) f[x] = s.pw[abs(r0 + g + 8 * (x >> 1) - (q0 + 8 * j + 2 * tg + (x & 1)))];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int t = r0 + g + 8 * (x >> 1), i = q0 + 8 * j + 2 * tg + (x & 1);
+                        const float v = (acc[j][x] + low[j][x]) * (p.sp * f[x]);
+                        s.P[t * Sm::LP + i] = (rev ? i >= t : i <= t) ? v : 0.f;
+                    }
+                }
             }
         }
         // out = e o (a S) + P c: 16 rows and CB / 2 columns, a S before P is there
@@ -225,15 +243,13 @@ __global__ void __launch_bounds__(kThreads) sfda_linear_f32_kernel(const Dev dev
         {   // S <- g^n S + (w o b)^T c.  Weak decays through g^n - 1, whose rounding is not the same relative error chunk
             // after chunk.
             float acc[TS][4] = {}, low[TS][4] = {};
-            const float x = (float)n * ld, gm = x > -0.5f ? expm1f(x) : expf(x);
 #pragma unroll 2
             for (int k0 = 0; k0 < L; k0 += 8) {
                 float av[4];
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                     const int i = k0 + tg + 4 * (y >> 1);
-                    const float w = i < n ? p.sw * s.pw[rev ? i + 1 : max(n - 1 - i, 0)] : 0.f;
-                    av[y] = w * sb[i * Sm::LA + 16 * wr + g + 8 * (y & 1)];
+                    av[y] = s.w[buf][i] * sb[i * Sm::LA + 16 * wr + g + 8 * (y & 1)];
                 }
 #pragma unroll
                 for (int j = 0; j < TS; ++j) {
@@ -246,7 +262,7 @@ __global__ void __launch_bounds__(kThreads) sfda_linear_f32_kernel(const Dev dev
             for (int j = 0; j < TS; ++j)
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
-                    st[j][y] = (x > -0.5f ? fmaf(st[j][y], gm, st[j][y]) : st[j][y] * gm) + (acc[j][y] + low[j][y]);
+                    st[j][y] = (weak ? fmaf(st[j][y], gm, st[j][y]) : st[j][y] * gm) + (acc[j][y] + low[j][y]);
             keep_copy();
         }
     }
@@ -277,8 +293,8 @@ cudaError_t launch_one(const LinearArgs &a, const Dev &d, int count, cudaStream_
 {
     // wide blocks of columns repeat P less often, narrow ones fill the SMs
     const long long chains = (long long)a.B * a.H * count;
-    if (chains * (DC / 32) <= 148) return launch_block<DA, DC, 16>(a, d, count, stream);
-    if (chains * (DC / 64) <= 148) return launch_block<DA, DC, 32>(a, d, count, stream);
+    if (chains * (DC / 16) <= 148) return launch_block<DA, DC, 16>(a, d, count, stream);
+    if (chains * (DC / 32) <= 148) return launch_block<DA, DC, 32>(a, d, count, stream);
     return launch_block<DA, DC, 64>(a, d, count, stream);
 }
 
