@@ -67,12 +67,6 @@ __global__ void __launch_bounds__(kThreads) sfda_group_norm_kernel(const Dev p)
         const int e = (lane + j * p.lanes) * V;
         in[j] = have && e < p.D;
         ch[j] = in[j] ? grp * p.D + e : 0;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            w[j][i] = p.weight ? __ldg(p.weight + ch[j] + i) : 1.f;
-            b[j][i] = p.bias ? __ldg(p.bias + ch[j] + i) : 0.f;
-            if (kBackward) aw[j][i] = ab[j][i] = 0.f;
-        }
     }
     const T *px = static_cast<const T *>(p.x), *pg = static_cast<const T *>(p.gate), *pd = static_cast<const T *>(p.dy);
     const long long step = (long long)gridDim.x * p.rb;
@@ -93,6 +87,17 @@ __global__ void __launch_bounds__(kThreads) sfda_group_norm_kernel(const Dev p)
         }
     };
     fetch((long long)blockIdx.x * p.rb + sub);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            w[j][i] = 1.f;
+            b[j][i] = 0.f;
+            if (kBackward) aw[j][i] = ab[j][i] = 0.f;
+        }
+        if (p.weight) ld_vec(p.weight + ch[j], w[j]);
+        if (p.bias) ld_vec(p.bias + ch[j], b[j]);
+    }
     for (long long base = (long long)blockIdx.x * p.rb; base < p.rows; base += step) {
         const long long row = base + sub;
         const bool live = have && row < p.rows;

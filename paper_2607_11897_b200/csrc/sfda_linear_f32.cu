@@ -4,7 +4,7 @@
 // in order, the next chunk's tiles on their way while it works: P = (a b^T) o D, out = P c + e o (a S), S <- g^n S + (w o b)^T c.  The columns of a state never interact, so blocks
 // of columns of a pair are independent (each repeats P); they are what keeps the SMs busy when there are few pairs.
 // All products run on the warp-level tensor cores with both operands split into two tf32 parts (hi hi + hi lo + lo hi:
-// 21 bits of each operand, sums in fp32).  The state stays in the accumulators of the warps that own its rows; a copy in
+// 22 bits of each operand, sums in fp32).  The state stays in the accumulators of the warps that own its rows; a copy in
 // shared memory is the operand of a S.
 //
 // A value of c that is not finite would reach earlier tokens of its chunk through 0 * NaN, since masked entries of P are
@@ -25,8 +25,11 @@ constexpr int kNever = 0x7fffffff;
 
 __device__ __forceinline__ void split_tf32(float x, uint32_t &hi, uint32_t &lo)
 {
-    hi = __float_as_uint(x) & 0xffffe000u;                 // the tensor core reads 10 mantissa bits: cut, not rounded,
-    lo = __float_as_uint(x - __uint_as_float(hi));         // so that the rest is exact
+    // The tensor core cuts its operands off at 10 mantissa bits.  Half a step added before that makes it a rounding for the high
+    // part (ties away from zero), which leaves 2^-12; the low part is cut at 2^-10 of that, either sign as often as the other.
+    // (A NaN of all ones loses its exponent in the high part; the difference is a NaN still, and stays one.)
+    hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+    lo = __float_as_uint(x - __uint_as_float(hi));
 }
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2])
 {
