@@ -327,10 +327,10 @@ Shape shape_of(int C, int G, int dtype)
     s.blocks_y = (G + s.gb - 1) / s.gb;
     return s;
 }
-// CTAs over the rows: a few waves of the device, so that the backward's partial sums stay few
-unsigned blocks_over_rows(const Shape &s, long long rows, int waves)
+// CTAs over the rows: a few waves of the device, and at least `each` steps for a CTA, so that the backward's partial sums stay few
+unsigned blocks_over_rows(const Shape &s, long long rows, int waves, int each)
 {
-    const long long want = (rows + s.rb - 1) / s.rb, most = (148ll * waves + s.blocks_y - 1) / s.blocks_y;
+    const long long want = (rows + (long long)s.rb * each - 1) / ((long long)s.rb * each), most = (148ll * waves + s.blocks_y - 1) / s.blocks_y;
     return (unsigned)(want < most ? want : most);
 }
 constexpr int kForwardWaves = 8, kBackwardWaves = 8;
@@ -375,7 +375,7 @@ bool group_norm_supported(int C, int G, int dtype) { return shape_of(C, G, dtype
 cudaError_t launch_group_norm(const GroupNormArgs &a, cudaStream_t stream, int *launches)
 {
     const Shape s = shape_of(a.C, a.G, a.dtype);
-    const dim3 grid(blocks_over_rows(s, a.rows, kForwardWaves), s.blocks_y);
+    const dim3 grid(blocks_over_rows(s, a.rows, kForwardWaves, 1), s.blocks_y);
     const Dev p = dev_of(a, s);
     const cudaError_t e = a.dtype == 1 ? launch_v<__nv_bfloat16, false>(s, p, grid, stream) : launch_v<float, false>(s, p, grid, stream);
     if (e == cudaSuccess && launches) ++*launches;
@@ -392,9 +392,9 @@ size_t group_norm_backward_bytes(long long rows, int C)
 cudaError_t launch_group_norm_backward(const GroupNormArgs &a, void *workspace, cudaStream_t stream, int *launches)
 {
     const Shape s = shape_of(a.C, a.G, a.dtype);
-    const dim3 grid(blocks_over_rows(s, a.rows, kBackwardWaves), s.blocks_y);
     Dev p = dev_of(a, s);
     if (a.dweight || a.dbias) p.part = static_cast<float *>(workspace);
+    const dim3 grid(blocks_over_rows(s, a.rows, kBackwardWaves, p.part ? 4 : 1), s.blocks_y);
     cudaError_t e = a.dtype == 1 ? launch_v<__nv_bfloat16, true>(s, p, grid, stream) : launch_v<float, true>(s, p, grid, stream);
     if (e != cudaSuccess) return e;
     if (launches) ++*launches;

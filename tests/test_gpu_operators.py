@@ -252,6 +252,28 @@ def test_linear_offsets_past_32_bits():
     torch.cuda.empty_cache()
 
 
+def test_linear_results_do_not_depend_on_the_timing_of_the_roles():
+    """The bf16 kernel's roles hand chunks to one another; a development build pauses them at random after arrivals and waits, and
+    has to give the same bits: pairs that share a CTA, cut sequences, ends within a chunk, empty ones, both kinds of decays."""
+    from paper_2607_11897_b200 import binding
+    from paper_2607_11897_b200 import build as cuda_build
+    chaos = binding.load_library(cuda_build.build_variant("chaos", ["-DSFDA_WS_CHAOS"]))
+    mixed = [-0.001, -0.9, -0.1, -30.0, 0.0, -0.3]
+    cases = [Linear(50, 300, 6, decay=mixed, seed=40), Linear(3, 400, 6, 2, decay=mixed, lens=[400, 0, 129], seed=41),
+             Linear(1, 4000, 2, decay=[-0.01, -2.0], seed=42), Linear(40, 130, 6, dk=64, dv=128, decay=mixed, lens=[1, 130, 0, 128] * 10, seed=43)]
+    for x in cases:
+        want = x.forward() + tuple(x.backward())
+        plain, ws = binding.load(), x.workspace()
+        binding._LIB = chaos
+        try:
+            for _ in range(3):
+                got = x.forward(ws) + tuple(x.backward())
+                assert all(torch.equal(a, b) for a, b in zip(got, want))
+                assert sfda.sfda_workspace_status(ws) == 0
+        finally:
+            binding._LIB = plain
+
+
 # ---- linear attention: one token -------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("dk,dv", [(64, 64), (64, 128), (128, 64), (128, 128)])
