@@ -541,13 +541,22 @@ SFDA_API int sfda_backward_withheld_handoff(const void *q, const void *k, const 
  *         are left as they were; the final state is that after the last token, of a sequence of no tokens S0.
  *  S0     [B][H][d_k][d_v] float, or NULL (zero)
  *  o      [B][T][H][d_v] dtype
- *  S_T    [B][H][d_k][d_v] float, or NULL; may alias S0
+ *  S_T    [B][H][d_k][d_v] float, or NULL; may be S0 itself (no other output may overlap an input)
  *  workspace: sfda_linear_workspace_bytes(...) bytes of device scratch (NULL when that is 0), 16-byte aligned, clobbered;
  *         calls whose work may overlap on the GPU need one each.
  *
  * d_k, d_v in {64, 128}; any H, B and T >= 1.  SFDA_ERR_SHAPE where H_kv does not divide H, SFDA_ERR_VALUE for a scale that
  * is not finite.  The state and all sums are fp32.  A value that is not finite makes NaN of the outputs and states that
  * depend on it, and of nothing else.  The result is deterministic.
+ *
+ * SFDA_BF16: chunks of 128 tokens on tcgen05.  The masked scores and a copy of the state are rounded to bf16 as operands of the
+ * products that make an output (each as the output itself is); what goes into the state is in two bf16 parts, so that states
+ * are about 4e-6 (relative, in the 2-norm) off.  For heads with gamma >= 0.805 scores are scaled by up to 2^40 before the row's power
+ * of gamma takes that back, so |q . k| has to stay below 3e26.  With few sequences each is cut into stretches of time, whose
+ * states a first launch makes (the workspace holds them).  The workspace begins with the status word that sfda_workspace_status
+ * reads: every wait inside the kernel is bounded (seconds), and where one runs out the call's outputs are invalid and the status is
+ * SFDA_ERR_TIMEOUT.  No CTA waits for another one.
+ * SFDA_F32: chunks of 64 tokens, operands in two tf32 parts (22 bits), no workspace.
  */
 SFDA_API size_t sfda_linear_workspace_bytes(int B, int T, int H, int H_kv, int d_k, int d_v, int dtype);
 SFDA_API int sfda_linear_forward(const void *q, const void *k, const void *v, const float *log_decay, const int32_t *lens,
@@ -626,8 +635,8 @@ SFDA_API int sfda_rotary_turns(uint64_t *turns, int rot, double base, int scalin
  *  x, gate, y [rows][C] dtype (gate may be NULL)     weight, bias [C] float, or NULL (1 and 0)
  *  act       SFDA_ACT_NONE: the identity; SFDA_ACT_SILU: u / (1 + exp(-u))
  *  y may be x or gate.  mean and var (divided by C / G) are those of the row's group alone, so rows are independent: tokens of
- *  a causal model.  Any G that divides C; at most 65535 groups where they are wider than 8192 channels (4096 in fp32; 1024
- *  where C / G is not a multiple of 4).  SFDA_ERR_VALUE unless eps is positive and finite.
+ *  a causal model.  Any G that divides C; SFDA_ERR_UNSUPPORTED where
+ *  groups of more than a thousand channels are more than 65535.  SFDA_ERR_VALUE unless eps is positive and finite.
  *
  * sfda_group_norm_backward: the gradients from dy [rows][C] dtype:  dx, dgate [rows][C] dtype (dgate is required with a
  * gate and ignored without), dweight, dbias [C] float, either of which may be NULL.  dx may be dy, dgate may be gate.

@@ -2,21 +2,23 @@
 //
 // A CTA takes one (batch, head) pair of one pass, or a stretch of its time axis, and walks its chunks of 128 tokens:
 //
-//   A  = a b^T                 tcgen05, both operands as TMA left them
-//   P  = A o D                 registers; rounded to bf16, back into tensor memory as the operand of
-//   O2 = P c                   tcgen05 (c MN-major)
-//   O1 = a S                   tcgen05; S as a bf16 copy of the fp32 state
-//   U  = (w o b)^T c           tcgen05; w o b in two bf16 parts, so that the state keeps 2^-17 of it
-//   out = e o O1 + O2,   S <- g^n S + U      registers, fp32
+//   A = a b^T                        tcgen05, both operands as TMA left them
+//   P = A o D                        registers; rounded to bf16, back into tensor memory as an operand
+//   O = a S,  O += P c               tcgen05; S as a bf16 copy of the fp32 state, c MN-major
+//   U = (w o b)^T c                  tcgen05; w o b in two bf16 parts, through tensor memory (run_keys)
+//   out = e o O,  S <- g^n S + U     registers, fp32
 //
-// D, e and w are powers of one number per head, so they are tables and per-thread constants.  The state lives in the
-// registers of eight warps and takes U with fp32 additions: accumulators of the tensor core cut sums off instead of rounding
-// them, which over thousands of tokens would be a bias.  U does not depend on the state, so the serial chain from chunk to
-// chunk is only S <- g S + U, its bf16 copy and O1.
+// D, e and w are powers of one number per head, so they are tables and per-thread constants; `shares` says how e gets out of P.
+// The state lives in the registers of eight warps and takes U with fp32 additions: accumulators of the tensor core cut sums off
+// instead of rounding them, which over thousands of tokens would be a bias.  U does not depend on the state, so the serial chain from
+// chunk to chunk is S <- g S + U, its bf16 copy and a S.
 //
-// Bound by memory (a, b, c read once, out written once).  28 warps: TMA, MMA, output copies, one idle, eight each for P and the output, for the
-// state and for w o b.  Two stages of (a, b, c); the high part of w o b replaces b and the low part that, once the products that
-// read them are done, and 
+// Memory is the floor (a, b, c read once, out written once: B = 8, T = 8192, H = 32, d = 128 take 336 us at 6.5 TB/s).  28 warps: TMA,
+// MMA, output copies, one idle, eight each for P and the output, for the state and for w o b.  Two stages of b and c; one place for a,
+// loaded out of L2 as soon as a S is done with it; one for the output.  Measured 457 us (4.7 TB/s) in bursts and 538 us under
+// sustained load, when the clock falls: the chain P, P c, output of a chunk (5000 cycles) and the issue of its 10500 warp
+// instructions are what is left above memory.  Before: outputs stored by the warps themselves 841 us (32 rows of a warp lie in 32
+// lines), descriptors computed per instruction 668, w o b through shared memory 562 (its bandwidth is what the products compete for).
 #include <cuda.h>
 
 #include "sfda_common.cuh"
@@ -46,7 +48,9 @@ enum { B_FULL = 0, B_EMPTY = 2, B_FULLA = 4, B_EMPTYA, B_EMPTYO, B_A, B_QS, B_K,
 struct Pass {
     void *out;
     const float *s_in;
-    float *s_out, *seg;          // seg: [pairs][nseg - 1][DA][DC] what earlier stretches leave, from a zero state
+    float *s_out, *seg;          // seg: [pairs][nseg][DA][DC], where sequences are cut: what the stretches but the last leave (the
+                                 // first from s_in, the others from zero), and a copy of s_in: s_out may be s_in, and is
+                                 // written while other stretches of the pair begin
     int ma, mb, mc;              // tensor maps of a, b, c
     int sa, sb, sc;              // query heads that share a head of a, b, c
     int reverse, s_in_t, out_f32;
@@ -574,36 +578,46 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
         uint64_t s[N / 2];                     // two columns each
 #pragma unroll
         for (int x = 0; x < N / 2; ++x) s[x] = 0;
-        if (!kStates && mine) {
-            if (ps.s_in) {
-                const size_t at = (size_t)un.pair * DA * DC;
-                if (ps.s_in_t) {
+        if (mine) {
+            float *seg = ps.seg + (size_t)un.pair * p.nseg * DA * DC + (size_t)k * DC + c0;      // the thread's part of the pair's states
+            const bool copied = !kStates && p.nseg > 1;
+            if (un.seg == 0 && ps.s_in) {
+                const float *from = copied ? seg + (size_t)(p.nseg - 1) * DA * DC : ps.s_in + (size_t)un.pair * DA * DC + (size_t)k * DC + c0;
+                if (ps.s_in_t && !copied) {
+                    from = ps.s_in + (size_t)un.pair * DA * DC + (size_t)c0 * DA + k;
 #pragma unroll
-                    for (int x = 0; x < N; x += 2)
-                        s[x / 2] = two(ps.s_in[at + (size_t)(c0 + x) * DA + k], ps.s_in[at + (size_t)(c0 + x + 1) * DA + k]);
+                    for (int x = 0; x < N; x += 2) s[x / 2] = two(from[(size_t)x * DA], from[(size_t)(x + 1) * DA]);
                 } else {
 #pragma unroll
                     for (int x = 0; x < N; x += 4) {
-                        const float4 v = *reinterpret_cast<const float4 *>(ps.s_in + at + (size_t)k * DC + c0 + x);
+                        const float4 v = *reinterpret_cast<const float4 *>(from + x);
                         s[x / 2] = two(v.x, v.y);
                         s[x / 2 + 1] = two(v.z, v.w);
                     }
                 }
-            }
-#pragma unroll 1
-            for (int j = 0; j < un.seg; ++j) {
-                const int tok = un.tokens(p, j);
-                if (tok == 0) continue;
-                const float gn = expf((float)tok * ld);
-                const uint64_t gg = two(gn, gn);
-                const float *from = ps.seg + ((size_t)un.pair * (p.nseg - 1) + j) * DA * DC + (size_t)k * DC + c0;
+                if (kStates)
 #pragma unroll
-                for (int x = 0; x < N; x += 4) {
-                    const float4 v = __ldcg(reinterpret_cast<const float4 *>(from + x));
-                    s[x / 2] = fma2(gg, s[x / 2], two(v.x, v.y));
-                    s[x / 2 + 1] = fma2(gg, s[x / 2 + 1], two(v.z, v.w));
-                }
+                    for (int x = 0; x < N; x += 4) {
+                        float4 v;
+                        apart(s[x / 2], v.x, v.y);
+                        apart(s[x / 2 + 1], v.z, v.w);
+                        *reinterpret_cast<float4 *>(seg + (size_t)(p.nseg - 1) * DA * DC + x) = v;
+                    }
             }
+            if (!kStates)
+#pragma unroll 1
+                for (int j = 0; j < un.seg; ++j) {
+                    const int tok = un.tokens(p, j);
+                    if (j > 0 && tok == 0) continue;
+                    const float gn = power(ld, tok);
+                    const uint64_t gg = two(gn, gn);
+#pragma unroll
+                    for (int x = 0; x < N; x += 4) {
+                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(seg + (size_t)j * DA * DC + x));
+                        s[x / 2] = fma2(gg, s[x / 2], two(v.x, v.y));
+                        s[x / 2 + 1] = fma2(gg, s[x / 2 + 1], two(v.z, v.w));
+                    }
+                }
         }
         const int chunks = un.hi - un.lo;
         nth += chunks > 0;
@@ -662,7 +676,7 @@ __device__ __forceinline__ void run_state(unsigned char *smem, Misc &mi, const P
                 arrive(mi, B_E);
             }
         }
-        float *to = kStates ? ps.seg + ((size_t)un.pair * (p.nseg - 1) + un.seg) * DA * DC
+        float *to = kStates ? ps.seg + ((size_t)un.pair * p.nseg + un.seg) * DA * DC
                             : un.seg == p.nseg - 1 && ps.s_out ? ps.s_out + (size_t)un.pair * DA * DC : nullptr;
         if (to && mine) {
             const int set = (nth - 1) % kSets;
@@ -946,7 +960,7 @@ size_t scratch_of(const LinearArgs &a, int passes, int d_k, int d_v, int *nseg)
 {
     const long long pairs = (long long)a.B * a.H;
     *nseg = stretches(pairs * passes, (a.T + C - 1) / C, 148);
-    return (size_t)passes * pairs * (*nseg - 1) * d_k * d_v * 4;
+    return *nseg == 1 ? 0 : (size_t)passes * pairs * *nseg * d_k * d_v * 4;
 }
 
 }  // namespace
@@ -991,7 +1005,7 @@ cudaError_t launch_linear_tc(const LinearArgs &a, const LinearPass *passes, int 
             const LinearPass &x = passes[at + i];
             Pass &y = p.pass[i];
             y.out = x.out; y.s_in = x.s_in; y.s_out = x.s_out;
-            y.seg = seg + i * each * (p.nseg - 1);
+            y.seg = seg + i * each * p.nseg;
             y.ma = map_of(x.a, x.Ha, DA); y.mb = map_of(x.b, x.Hb, DA); y.mc = map_of(x.c, x.Hc, DC);
             if (y.ma < 0 || y.mb < 0 || y.mc < 0 || (!x.out_f32 && !make_map(&p.out[i], x.out, a.B, a.T, a.H, DC)))
                 return cudaErrorInvalidValue;

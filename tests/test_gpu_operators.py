@@ -182,6 +182,22 @@ def test_linear_final_state_may_overwrite_the_initial_one():
         assert torch.equal(nothing, o)
 
 
+def test_linear_final_state_may_overwrite_the_initial_one_of_cut_sequences():
+    """Sequences that are cut into stretches of time, the last of them empty: its CTA writes the final state while others begin."""
+    for lens in ([4000], [10], [0], [2100]):
+        x = Linear(1, 4000, 2, lens=lens, decay=[-2.0 ** -12, -0.0], seed=44)
+        o, S = x.forward()
+        (wo, wS), _ = x.oracle()
+        assert off(o, wo) <= (BF16 if lens[0] else 0) and off(S, wS) <= STATE
+        ws, keep = x.workspace(), x.S0.clone()
+        assert ws.numel() > 256 + 4 * S.numel()
+        for _ in range(20):
+            x.S0.copy_(keep)
+            o2 = torch.zeros_like(o)
+            sfda.sfda_linear_forward(x.q, x.k, x.v, x.log_decay, x.lens, x.S0, o2, x.S0, x.scale, ws)
+            assert torch.equal(x.S0, S) and torch.equal(o2, o)
+
+
 def test_linear_pieces_of_a_sequence_continue_each_other():
     for dtype in DTYPES:
         x = Linear(1, 700, 2, dtype=dtype, seed=14)
