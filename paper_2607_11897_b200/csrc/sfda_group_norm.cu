@@ -278,8 +278,8 @@ __global__ void __launch_bounds__(kThreads) sfda_group_norm_wide_kernel(const De
                         pw[ch] = first ? dz * n : pw[ch] + dz * n;
                         pb[ch] = first ? dz : pb[ch] + dz;
                     }
+                } else {                                   // (both outputs here: they may lie over dy and the gate)
                     if (pg) st_val(static_cast<T *>(p.dgate), at, dy * z * slope);
-                } else {
                     st_val(static_cast<T *>(p.dx), at, rstd * (dn - s1 - n * s2));
                 }
             }

@@ -533,6 +533,42 @@ def test_group_norm_writes_over_its_input_and_keeps_rows_apart():
     assert torch.equal(z[~bad], y[~bad]) and torch.isnan(z[bad]).all()
 
 
+@pytest.mark.parametrize("C,groups", [(16384, 1), (5003, 1), (4096, 1), (3 * 1500, 3), (144, 4)])
+def test_group_norm_gradients_may_lie_over_their_inputs(C, groups):
+    x, w, b, gate, dy = norm_case(6, C, "bf16", True, True)
+    ws = torch.empty(sfda.sfda_group_norm_backward_workspace_bytes(6, C), device="cuda", dtype=torch.uint8)
+    want = [torch.empty_like(x), torch.empty(C, device="cuda"), torch.empty(C, device="cuda"), torch.empty_like(x)]
+    sfda.sfda_group_norm_backward(x, w, b, gate, dy, *want, groups, 1e-5, 1, ws)
+    dw, db = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    sfda.sfda_group_norm_backward(x, w, b, gate, dy, dy, dw, db, gate, groups, 1e-5, 1, ws)
+    assert all(torch.equal(i, j) for i, j in zip((dy, dw, db, gate), want))
+
+
+def test_operators_run_on_the_stream_that_is_named():
+    """Each on a stream of its own while the default one is busy: what it reads is written on that stream, right before."""
+    s = torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device="cuda")
+    x, w, b, gate, dy = norm_case(64, 256, "bf16", True, True)
+    q, k, pos, turns = rotary_case(2, 9, 4, 2, 64, 64, "bf16")
+    step = Linear(2, 1, 4, dk=64, dv=64, seed=45)
+    args = [t[:, 0].contiguous() for t in (step.q, step.k, step.v)]
+    results = []
+    for stream in (None, s):
+        y, q2, k2, S, o = torch.empty_like(x), torch.empty_like(q), torch.empty_like(k), step.S0.clone(), torch.empty(2, 4, 64, device="cuda", dtype=step.dt)
+        torch.cuda.synchronize()
+        if stream is not None:
+            for _ in range(5):
+                big = (big @ big).clamp_(-1, 1)
+        with torch.cuda.stream(stream):
+            x2, qq = x * 2, q * 2
+        sfda.sfda_group_norm(x2, w, b, gate, y, 4, 1e-5, 1, stream)
+        sfda.sfda_rotary(qq, k, pos, turns, q2, k2, 0, 1.0, False, stream)
+        sfda.sfda_linear_step(*args, step.log_decay, S, o, 1.0, stream)
+        torch.cuda.synchronize()
+        results.append((y, q2, k2, S, o))
+    assert all(torch.equal(i, j) for i, j in zip(*results))
+
+
 def test_group_norm_sums_are_the_same_bits_every_time_and_captured():
     x, w, b, gate, dy = norm_case(5000, 512, "bf16", True, True)
     ws = torch.empty(sfda.sfda_group_norm_backward_workspace_bytes(5000, 512), device="cuda", dtype=torch.uint8)
