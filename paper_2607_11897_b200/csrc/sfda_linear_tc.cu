@@ -991,14 +991,16 @@ cudaError_t launch_linear_tc(const LinearArgs &a, const LinearPass *passes, int 
         scratch_of(a, p.n_pass, DA, DC, &p.nseg);
         const int chunks = (a.T + C - 1) / C;
         p.cps = (chunks + p.nseg - 1) / p.nseg;
+        // one map for each tensor: inputs of different widths may begin at the same address
         const void *seen[4] = {};
-        int heads[4] = {}, maps = 0;
+        int heads[4] = {}, widths[4] = {}, maps = 0;
         auto map_of = [&](const void *x, int h, int d) {
             for (int i = 0; i < maps; ++i)
-                if (seen[i] == x && heads[i] == h) return i;
+                if (seen[i] == x && heads[i] == h && widths[i] == d) return i;
             if (maps == 4 || !make_map(&p.map[maps], x, a.B, a.T, h, d)) return -1;
             seen[maps] = x;
             heads[maps] = h;
+            widths[maps] = d;
             return maps++;
         };
         for (int i = 0; i < p.n_pass; ++i) {
