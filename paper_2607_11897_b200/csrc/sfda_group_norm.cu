@@ -103,8 +103,9 @@ __global__ void __launch_bounds__(kThreads) sfda_group_norm_kernel(const Dev p)
             b[j][i] = 0.f;
             if (kBackward) aw[j][i] = ab[j][i] = 0.f;
         }
-        if (p.weight) ld_vec(p.weight + ch[j], w[j]);
-        if (p.bias) ld_vec(p.bias + ch[j], b[j]);
+        // (lanes without a channel keep 1 and 0: their zeros go into the group's sums, and 0 times a parameter that is not finite is none)
+        if (p.weight && in[j]) ld_vec(p.weight + ch[j], w[j]);
+        if (p.bias && in[j]) ld_vec(p.bias + ch[j], b[j]);
     }
     for (long long base = (long long)blockIdx.x * p.rb; base < p.rows; base += step) {
         const long long row = base + sub;

@@ -42,3 +42,39 @@ def test_linear_inputs_may_be_views_of_one_buffer(pair, d_k, d_v, dtype):
 
     for name, a, b in zip(("o", "S_T", "dq", "dk", "dv", "dS0"), run(views), run(alone)):
         assert torch.equal(a, b), name
+
+
+# ---- group norm ------------------------------------------------------------------------------------------------------
+def norm_inputs(rows, C, dtype, seed, mean=0.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    return (r(rows, C) + mean).to(DTYPES[dtype]), r(C), r(C), r(rows, C).to(DTYPES[dtype]), r(rows, C).to(DTYPES[dtype])
+
+
+def norm(x, w, b, gate, dy, groups, eps, act):
+    """(y, dx, dweight, dbias, dgate)"""
+    e, C = torch.empty_like, x.shape[1]
+    y, dx, dw, db, dg = e(x), e(x), e(w), e(w), None if gate is None else e(x)
+    sfda.sfda_group_norm(x, w, b, gate, y, groups, eps, act)
+    sfda.sfda_group_norm_backward(x, w, b, gate, dy, dx, dw, db, dg, groups, eps, act,
+                                  scratch(sfda.sfda_group_norm_backward_workspace_bytes(x.shape[0], C)))
+    return y, dx, dw, db, dg
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("C,groups", [(288, 3), (252, 7), (1500, 3), (2 * 1100, 2), (2 * 5003, 2), (256, 2)])
+def test_group_norm_parameters_that_are_not_finite_stay_in_their_group(C, groups, gated, act, dtype):
+    """The first channel's weight or bias is not finite: results of the other groups keep their bits, whether or not a group fills
+    the lanes that work on it."""
+    x, w, b, gate, dy = norm_inputs(5, C, dtype, 2)
+    gate = gate if gated else None
+    D, clean = C // groups, norm(x, w, b, gate, dy, groups, 1e-5, act)
+    for value in (float("inf"), float("nan")):
+        for which in (0, 1):
+            params = [w.clone(), b.clone()]
+            params[which][0] = value
+            for name, got, want in zip(("y", "dx", "dweight", "dbias", "dgate"), norm(x, *params, gate, dy, groups, 1e-5, act), clean):
+                if want is not None:
+                    assert torch.equal(got[..., D:], want[..., D:]), (name, value, which)
