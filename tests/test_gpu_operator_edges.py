@@ -78,3 +78,43 @@ def test_group_norm_parameters_that_are_not_finite_stay_in_their_group(C, groups
             for name, got, want in zip(("y", "dx", "dweight", "dbias", "dgate"), norm(x, *params, gate, dy, groups, 1e-5, act), clean):
                 if want is not None:
                     assert torch.equal(got[..., D:], want[..., D:]), (name, value, which)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("eps", [1e-5, 1e-12])
+@pytest.mark.parametrize("D", [36, 96, 100, 128, 129, 500, 5003])
+def test_group_norm_of_constant_groups_is_the_bias_at_any_width(D, eps, dtype):
+    """A group of one value has no deviation, however large the value and small eps.  bf16: a sum of D equal values is exact (8 + 13
+    bits), and so is the mean.  fp32: the sum is off by its roundings, so that all differences are the same j units in the last place
+    of the value, j < 100 (45 additions in a row at most, half a unit each, in a binade that may be half as wide); D j < 2^24, so
+    their own mean is exact and what is left is zero."""
+    g = torch.Generator(device="cuda").manual_seed(D)
+    c = torch.exp(torch.rand(64, 2, 1, device="cuda", generator=g) * 23.0 - 11.5) * (torch.randint(0, 2, (64, 2, 1), device="cuda", generator=g) * 2 - 1)
+    x = c.expand(64, 2, D).reshape(64, 2 * D).to(DTYPES[dtype])
+    w, b = torch.randn(2 * D, device="cuda", generator=g), torch.randn(2 * D, device="cuda", generator=g)
+    y = torch.empty_like(x)
+    sfda.sfda_group_norm(x, w, b, None, y, 2, eps)
+    assert torch.equal(y, b.to(x.dtype).expand(64, 2 * D))
+    # n = 0: dweight vanishes, dx = (dn - mean of dn) / sqrt(eps)
+    dy = torch.randn(64, 2 * D, device="cuda", generator=g).to(x.dtype)
+    _, dx, dw, db, _ = norm(x, w, b, None, dy, 2, eps, 0)
+    assert not dw.any()
+    dn = (dy.double() * w.double()).view(64, 2, D)
+    want = ((dn - dn.mean(-1, keepdim=True)) / eps ** 0.5).view(64, 2 * D)
+    # a mean and three operations in fp32: 2e-6, as for all shapes; one rounding of half a step for bf16
+    assert (dx.double() - want).norm() / want.norm() <= (2e-6 if dtype == "f32" else torch.finfo(torch.bfloat16).eps / 2)
+
+
+def test_group_norm_of_a_variance_below_its_rounding_is_finite():
+    """The variance about the first mean is less than that about the true one by the square of the means' distance.  Where nearly all
+    of it is that distance (groups of one value, or of one value but for one unit in the last place), rounding may leave less than
+    nothing, and an eps of 1e-12 does not lift it above zero."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    for rows, D in ((4096, 500), (4096, 1000), (64, 1 << 18)):
+        c = torch.exp(torch.rand(rows, 1, device="cuda", generator=g) * 6.9 + 6.9).expand(rows, D).contiguous()
+        one = c.clone()
+        one[:, D // 3] = torch.nextafter(one[:, D // 3], torch.full((), float("inf"), device="cuda"))
+        for x in (c, one):
+            y = torch.empty_like(x)
+            sfda.sfda_group_norm(x, None, None, None, y, 1, 1e-12)
+            assert torch.isfinite(y).all(), (rows, D)
