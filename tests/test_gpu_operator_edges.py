@@ -1,9 +1,11 @@
 """Calls of the operators beside the recurrence that their documentation allows and that are easy to get wrong: inputs that share an
 address, parameters that are not finite, groups of one value, named streams."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2607_11897_b200 as sfda
+from oracle import operators as op
 
 pytestmark = pytest.mark.gpu
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
@@ -118,3 +120,19 @@ def test_group_norm_of_a_variance_below_its_rounding_is_finite():
             y = torch.empty_like(x)
             sfda.sfda_group_norm(x, None, None, None, y, 1, 1e-12)
             assert torch.isfinite(y).all(), (rows, D)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("D", [36, 100, 128, 500, 2048, 5003])
+def test_group_norm_of_unit_deviations_about_a_large_mean(D, gated):
+    """Deviations of 1 about 4096 in fp32, the forward and the gradients.  Differences from the first mean are exact (multiples of 2^-12
+    below 2^3), and their own mean takes off what that one's rounding (up to some 2^-12) left: so what holds for a mean of 0
+    holds here, a sum and a dozen operations in fp32, 2e-6.  Without the second mean n is off by about 1e-4."""
+    x, w, b, gate, dy = norm_inputs(20, 2 * D, "f32", 3, mean=4096.0)
+    gate = gate if gated else None
+    f = lambda t: None if t is None else t.double().cpu().numpy()  # noqa: E731
+    want = (op.group_norm(f(x), f(w), f(b), f(gate), 2, 1e-5, True), *op.group_norm_backward(f(x), f(w), f(b), f(gate), f(dy), 2, 1e-5, True))
+    # (sums over rows partly cancel: four times as much, as for all shapes)
+    for name, got, y, t in zip(("y", "dx", "dweight", "dbias", "dgate"), norm(x, w, b, gate, dy, 2, 1e-5, 1), want, (2e-6, 2e-6, 8e-6, 8e-6, 2e-6)):
+        if y is not None:
+            assert np.linalg.norm(f(got) - y) <= t * np.linalg.norm(y), name
