@@ -136,3 +136,60 @@ def test_group_norm_of_unit_deviations_about_a_large_mean(D, gated):
     for name, got, y, t in zip(("y", "dx", "dweight", "dbias", "dgate"), norm(x, w, b, gate, dy, 2, 1e-5, 1), want, (2e-6, 2e-6, 8e-6, 8e-6, 2e-6)):
         if y is not None:
             assert np.linalg.norm(f(got) - y) <= t * np.linalg.norm(y), name
+
+
+# ---- named streams -----------------------------------------------------------------------------------------------------
+B, T, H, D = 2, 150, 4, 64
+
+
+def stream_calls():
+    """name: (inputs, outputs, call): every entry point that enqueues work, on given inputs and outputs and a stream."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    r = lambda *s: torch.randn(*s, device="cuda", generator=g).bfloat16()  # noqa: E731
+    q, k, v, d_o = (r(B, T, H, D) for _ in range(4))
+    ld, w, b = -torch.rand(H, device="cuda", generator=g), torch.randn(H * D, device="cuda", generator=g), torch.randn(H * D, device="cuda", generator=g)
+    state = torch.randn(B, H, D, D, device="cuda", generator=g)
+    pos, turns = torch.arange(T, device="cuda", dtype=torch.int32).repeat(B, 1), sfda.sfda_rotary_turns(D).cuda()
+    e, sizes = torch.empty_like, (B, T, H, H, D, D, sfda.SFDA_BF16)
+    fws, bws = scratch(sfda.sfda_linear_workspace_bytes(*sizes)), scratch(sfda.sfda_linear_backward_workspace_bytes(*sizes))
+    x, gate, dy = (t.view(B * T, H * D) for t in (q, k, v))
+    nws = scratch(sfda.sfda_group_norm_backward_workspace_bytes(B * T, H * D))
+    one = [t[:, 0].contiguous() for t in (q, k, v)]
+    return {
+        "linear_forward": ([q, k, v, state], [e(q), e(state)],
+                           lambda i, o, s: sfda.sfda_linear_forward(*i[:3], ld, None, i[3], *o, 0.5, fws, s)),
+        "linear_backward": ([q, k, v, state, d_o], [e(q), e(k), e(v), e(state)],
+                            lambda i, o, s: sfda.sfda_linear_backward(*i[:3], ld, None, i[3], i[4], None, *o, 0.5, bws, s)),
+        "linear_step": (one + [state], [e(one[0])], lambda i, o, s: sfda.sfda_linear_step(*i[:3], ld, i[3], o[0], 0.5, s)),
+        "rotary": ([q, k], [e(q), e(k)], lambda i, o, s: sfda.sfda_rotary(*i, pos, turns, *o, 0, 1.0, False, s)),
+        "group_norm": ([x, gate], [e(x)], lambda i, o, s: sfda.sfda_group_norm(i[0], w, b, i[1], o[0], H, 1e-5, 1, s)),
+        "group_norm_backward": ([x, gate, dy], [e(x), e(w), e(w), e(x)],
+                                lambda i, o, s: sfda.sfda_group_norm_backward(i[0], w, b, i[1], i[2], *o, H, 1e-5, 1, nws, s)),
+    }
+
+
+@pytest.mark.parametrize("name", ["linear_forward", "linear_backward", "linear_step", "rotary", "group_norm", "group_norm_backward"])
+def test_calls_wait_for_the_stream_that_is_named(name):
+    """The stream is held up before it writes the inputs; a call on it sees them, one that went to the current stream would read what
+    lay there before.  Outputs, inputs and scratch are made, and the device is idle, before the stream is held up, and all stay alive
+    until it is done."""
+    values, out, call = stream_calls()[name]
+    inputs = [t.clone() for t in values]
+    call(inputs, out, None)
+    want = [t.clone() for t in inputs + out]
+    for t in inputs:
+        t.fill_(7.0)
+    for t in out:
+        t.fill_(-3.0)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(40_000_000)                            # 20 ms or more
+        for t, y in zip(inputs, values):
+            t.copy_(y)
+    assert torch.cuda.current_stream() != s and not s.query()
+    call(inputs, out, s)
+    assert not s.query()
+    s.synchronize()
+    for a, b in zip(inputs + out, want):
+        assert torch.equal(a, b)
