@@ -20,6 +20,7 @@
 // instructions are what is left above memory.  Before: outputs stored by the warps themselves 841 us (32 rows of a warp lie in 32
 // lines), descriptors computed per instruction 668, w o b through shared memory 562 (its bandwidth is what the products compete for).
 #include <cuda.h>
+#include <stdlib.h>
 
 #include "sfda_common.cuh"
 #include "sfda_linear.h"
@@ -64,6 +65,9 @@ struct alignas(64) Params {
     const int *lens;
     uint32_t *status;
     int n_pass, T, H, pairs, nseg, cps, units, clear;     // cps: chunks of a stretch; clear: the call's first launch
+#ifdef SFDA_WS_CHAOS
+    int withhold;
+#endif
 };
 
 // Shared memory: a, two stages of b and c, the bf16 state, the output on its way out, then the small things.
@@ -76,6 +80,9 @@ struct Misc {
     unsigned long long bars[kBars];
     uint32_t tmem;
     volatile int abort;
+#ifdef SFDA_WS_CHAOS
+    int withhold;
+#endif
     int any[kSets];
     alignas(16) float pw[31 + C];// the powers of g that make P (see run_p)
     int first[kSets][128];      // by value column: the first token (in the pass's order) whose value was not finite.  Three
@@ -88,11 +95,20 @@ constexpr int kSmem = Layout<DA, DC>::kMisc + (int)sizeof(Misc);
 // at a time; after kTries of them (seconds), or when another wait of the CTA has given up, it gives up and says so.  A few
 // instructions, for it is inlined at every wait: the loops of all roles have to stay in the SM's instruction cache together.
 constexpr int kTries = 1 << 17;
+#ifdef SFDA_WS_CHAOS
+// Development builds only: with SFDA_WITHHOLD_LINEAR in the environment no warp arrives at the barrier of that number, and the limit is
+// short (milliseconds), so that waits run out.
+__device__ __forceinline__ bool withheld(const Misc &mi, int bar) { return mi.withhold == bar; }
+__device__ __forceinline__ int tries(const Misc &mi) { return mi.withhold < 0 ? kTries : 1 << 9; }
+#else
+__device__ __forceinline__ bool withheld(const Misc &, int) { return false; }
+__device__ __forceinline__ int tries(const Misc &) { return kTries; }
+#endif
 __device__ __forceinline__ bool wait_warp(Misc &mi, int bar, int k)
 {
     const uint32_t addr = smem_u32(&mi.bars[bar]), parity = (uint32_t)k & 1u;
 #pragma unroll 1
-    for (int n = 0; n < kTries; ++n) {
+    for (int n = 0; n < tries(mi); ++n) {
         uint32_t ok;
         asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}\n"
                      : "=r"(ok)
@@ -120,6 +136,7 @@ __device__ __forceinline__ bool ready(Misc &mi, int bar, int k)
 __device__ __forceinline__ void arrive(Misc &mi, int bar)
 {
     chaos(bar);
+    if (withheld(mi, bar)) return;
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&mi.bars[bar])) : "memory");
 }
 __device__ __forceinline__ bool elect_one()
@@ -817,6 +834,9 @@ __global__ void __launch_bounds__(kThreads, 1) sfda_linear_tc_kernel(const __gri
         const int counts[kBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 256, 1, 256, 1, 256, 256, 256, 256};
         for (int i = 0; i < kBars; ++i) mbar_init(&mi.bars[i], counts[i]);
         mi.abort = 0;
+#ifdef SFDA_WS_CHAOS
+        mi.withhold = p.withhold;
+#endif
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (p.clear && blockIdx.x == 0) *p.status = 0;      // what an earlier call left there; a wait runs out much later
     }
@@ -983,6 +1003,9 @@ cudaError_t launch_linear_tc(const LinearArgs &a, const LinearPass *passes, int 
     p.H = a.H;
     p.pairs = a.B * a.H;
     p.clear = 1;
+#ifdef SFDA_WS_CHAOS
+    p.withhold = getenv("SFDA_WITHHOLD_LINEAR") ? atoi(getenv("SFDA_WITHHOLD_LINEAR")) : -1;
+#endif
     float *seg = reinterpret_cast<float *>(static_cast<char *>(workspace) + 256);
     for (int at = 0; at < count;) {
         p.n_pass = group_of(passes + at, count - at);

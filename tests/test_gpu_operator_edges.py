@@ -193,3 +193,49 @@ def test_calls_wait_for_the_stream_that_is_named(name):
     s.synchronize()
     for a, b in zip(inputs + out, want):
         assert torch.equal(a, b)
+
+
+# ---- waits that run out ------------------------------------------------------------------------------------------------
+@pytest.fixture(scope="module")
+def development():
+    from paper_2607_11897_b200 import binding
+    from paper_2607_11897_b200 import build as cuda_build
+    return binding.load_library(cuda_build.build_variant("chaos", ["-DSFDA_WS_CHAOS"]))
+
+
+# barriers that warps arrive at (their places in sfda_linear_tc.cu): the output's place, the keys, P, the output in tensor memory and in
+# shared memory, the state, and e of heads that forget fast
+@pytest.mark.parametrize("barrier", [6, 9, 11, 13, 14, 15, 16])
+@pytest.mark.parametrize("sizes", [(3, 300, 6, 6, 128, 128), (1, 4000, 2, 1, 128, 128), (2, 400, 4, 2, 64, 128)])
+def test_linear_waits_that_run_out_are_reported_and_leave_the_context_usable(development, monkeypatch, sizes, barrier):
+    """The bf16 kernel of a development build with one of its roles' arrivals withheld and a limit of milliseconds: all roles leave, the
+    kernel ends, the status says so, of whole and of cut sequences (two launches) and of gradients.  The same call with the
+    plain build and the same workspace gives its bits again and clears the status."""
+    from paper_2607_11897_b200 import binding
+    B, T, H, H_kv, d_k, d_v = sizes
+    g = torch.Generator(device="cuda").manual_seed(5)
+    r = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    q, k, v, d_o = r(B, T, H, d_k).bfloat16(), (0.1 * r(B, T, H_kv, d_k)).bfloat16(), r(B, T, H_kv, d_v).bfloat16(), r(B, T, H, d_v).bfloat16()
+    ld, S0 = torch.tensor([-0.001, -0.9, -0.1, -30.0, 0.0, -0.3][:H], device="cuda"), r(B, H, d_k, d_v)
+    size = sizes + (sfda.SFDA_BF16,)
+    fws, bws = scratch(sfda.sfda_linear_workspace_bytes(*size)), scratch(sfda.sfda_linear_backward_workspace_bytes(*size))
+
+    def run():
+        o, S, grads = torch.zeros_like(d_o), torch.zeros_like(S0), [torch.zeros_like(t) for t in (q, k, v, S0)]
+        sfda.sfda_linear_forward(q, k, v, ld, None, S0, o, S, 0.5, fws)
+        sfda.sfda_linear_backward(q, k, v, ld, None, S0, d_o, None, *grads, 0.5, bws)
+        torch.cuda.synchronize()
+        return [o, S] + grads
+
+    want = run()
+    with monkeypatch.context() as m:
+        m.setattr(binding, "_LIB", development)
+        m.setenv("SFDA_WITHHOLD_LINEAR", str(barrier))
+        run()
+        for ws in (fws, bws):
+            with pytest.raises(sfda.SfdaError) as e:
+                sfda.sfda_workspace_status(ws)
+            assert e.value.status == -7
+    for _ in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(run(), want))
+        assert sfda.sfda_workspace_status(fws) == 0 and sfda.sfda_workspace_status(bws) == 0
