@@ -557,8 +557,8 @@ SFDA_API int sfda_backward_withheld_handoff(const void *q, const void *k, const 
  * states a first launch makes (the workspace holds them).  The workspace begins with the status word that sfda_workspace_status
  * reads: every wait inside the kernel is bounded (seconds), and where one runs out the call's outputs are invalid and the status is
  * SFDA_ERR_TIMEOUT.  No CTA waits for another one.
- * SFDA_F32: chunks of 64 tokens, operands in two tf32 parts (22 bits); no waits, no status word, and a workspace only for the
- * gradients of shared heads.
+ * SFDA_F32: chunks of 64 tokens, operands in two tf32 parts (22 bits), magnitudes from 2^128 - 2^116 on as if they were not
+ * finite; no waits, no status word, and a workspace only for the gradients of shared heads.
  */
 SFDA_API size_t sfda_linear_workspace_bytes(int B, int T, int H, int H_kv, int d_k, int d_v, int dtype);
 SFDA_API int sfda_linear_forward(const void *q, const void *k, const void *v, const float *log_decay, const int32_t *lens,

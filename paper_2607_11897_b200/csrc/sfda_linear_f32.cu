@@ -9,9 +9,7 @@
 //
 // A value of c that is not finite would reach earlier tokens of its chunk through 0 * NaN, since masked entries of P are
 // zeros of a dense product.  Such a value is taken as zero, and its column's outputs from that token on, and its column of
-// the state, are NaN instead.
-#include <float.h>
-
+// the state, are NaN instead.  The same holds for the largest finite values (from 2^128 - 2^116 on), whose high part rounds to infinity.
 #include "sfda_common.cuh"
 #include "sfda_linear.h"
 #include "sfda_tc_ptx.cuh"
@@ -22,6 +20,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int L = 64;            // tokens per chunk
 constexpr int kNever = 0x7fffffff;
+constexpr float kMost = 0x1.ffdffep127f;     // the largest value whose high part is finite
 
 __device__ __forceinline__ void split_tf32(float x, uint32_t &hi, uint32_t &lo)
 {
@@ -154,7 +153,7 @@ __global__ void __launch_bounds__(kThreads) sfda_linear_f32_kernel(const Dev dev
             const int r = x / (CB / 4), d = x % (CB / 4) * 4;
 #pragma unroll
             for (int y = 0; y < 4; ++y)
-                if (!(fabsf(sc[r * Sm::LC + d + y]) <= FLT_MAX)) {
+                if (!(fabsf(sc[r * Sm::LC + d + y]) <= kMost)) {
                     sc[r * Sm::LC + d + y] = 0.f;
                     atomicMin(&s.first[d + y], rev ? len - 1 - (t0 + r) : t0 + r);
                 }

@@ -46,6 +46,42 @@ def test_linear_inputs_may_be_views_of_one_buffer(pair, d_k, d_v, dtype):
         assert torch.equal(a, b), name
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_linear_largest_finite_values_do_not_reach_earlier_tokens(sign, dtype):
+    """The type's largest and lowest value in v, q and d_o: masked scores are zeros of a dense product, and zero times it is zero.  What does
+    not depend on the entry has the bits of the clean run."""
+    T, t, c, dt = 300, 140, 17, DTYPES[dtype]
+    g = torch.Generator(device="cuda").manual_seed(7)
+    clean = {n: torch.randn(1, T, 2, 64, device="cuda", generator=g).to(dt) for n in "qkvd"}
+    ld, sizes = torch.tensor([-0.01, -0.7], device="cuda"), (1, T, 2, 2, 64, 64, int(dtype == "bf16"))
+
+    def run(x):
+        o, S = torch.empty_like(x["v"]), torch.empty(1, 2, 64, 64, device="cuda")
+        sfda.sfda_linear_forward(x["q"], x["k"], x["v"], ld, None, None, o, S, 0.5, scratch(sfda.sfda_linear_workspace_bytes(*sizes)))
+        grads = [torch.empty_like(x["q"]) for _ in range(3)] + [torch.empty_like(S)]
+        sfda.sfda_linear_backward(x["q"], x["k"], x["v"], ld, None, None, x["d"], None, *grads, 0.5,
+                                  scratch(sfda.sfda_linear_backward_workspace_bytes(*sizes)))
+        return [o, S] + grads
+
+    want = run(clean)
+    for h in (0, 1):
+        for name in "vqd":
+            x = dict(clean)
+            x[name] = clean[name].clone()
+            x[name][0, t, h, c] = sign * torch.finfo(dt).max
+            reach = [torch.zeros_like(y, dtype=torch.bool) for y in want]
+            o, S, dq, dk, dv, dS = reach
+            if name == "v":
+                o[0, t:, h, c] = S[0, h, :, c] = dq[0, t:, h] = dk[0, t, h] = True
+            elif name == "q":
+                o[0, t, h] = dk[0, :t + 1, h, c] = dv[0, :t + 1, h] = dS[0, h, c] = True
+            else:
+                dq[0, t, h] = dk[0, :t + 1, h] = dv[0, :t + 1, h, c] = dS[0, h, :, c] = True
+            for n, (got, y, r) in enumerate(zip(run(x), want, reach)):
+                assert torch.equal(got[~r], y[~r]), (name, h, n)
+
+
 # ---- group norm ------------------------------------------------------------------------------------------------------
 def norm_inputs(rows, C, dtype, seed, mean=0.0):
     g = torch.Generator(device="cuda").manual_seed(seed)
