@@ -82,6 +82,47 @@ def test_linear_largest_finite_values_do_not_reach_earlier_tokens(sign, dtype):
                 assert torch.equal(got[~r], y[~r]), (name, h, n)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("T,t", [(300, 140), (2500, 1500)])
+def test_linear_values_that_are_not_finite_at_weak_decays_and_in_cut_sequences(T, t, value, dtype):
+    """Heads that hardly forget, whose scores the bf16 kernel scales by the column, and sequences that it cuts into stretches."""
+    c, dt = 17, DTYPES[dtype]
+    g = torch.Generator(device="cuda").manual_seed(8)
+    clean = {n: torch.randn(1, T, 2, 64, device="cuda", generator=g).to(dt) for n in "qkvd"}
+    clean["k"] = (0.1 * clean["k"]).to(dt)
+    ld, sizes = torch.tensor([-0.01, 0.0], device="cuda"), (1, T, 2, 2, 64, 64, int(dtype == "bf16"))
+    S0 = torch.randn(1, 2, 64, 64, device="cuda", generator=g)
+
+    def run(x):
+        o, S = torch.empty_like(x["v"]), torch.empty_like(S0)
+        sfda.sfda_linear_forward(x["q"], x["k"], x["v"], ld, None, S0, o, S, 0.5, scratch(sfda.sfda_linear_workspace_bytes(*sizes)))
+        grads = [torch.empty_like(x["q"]) for _ in range(3)] + [torch.empty_like(S)]
+        sfda.sfda_linear_backward(x["q"], x["k"], x["v"], ld, None, S0, x["d"], S0, *grads, 0.5,
+                                  scratch(sfda.sfda_linear_backward_workspace_bytes(*sizes)))
+        return [o, S] + grads
+
+    want = run(clean)
+    for h in (0, 1):
+        for name in "qkvd":
+            x = dict(clean)
+            x[name] = clean[name].clone()
+            x[name][0, t, h, c] = value
+            reach = [torch.zeros_like(y, dtype=torch.bool) for y in want]
+            o, S, dq, dk, dv, dS = reach
+            if name == "q":
+                o[0, t, h] = dk[0, :t + 1, h, c] = dv[0, :t + 1, h] = dS[0, h, c] = True
+            elif name == "k":
+                o[0, t:, h] = S[0, h, c] = dq[0, t:, h, c] = dv[0, t, h] = True
+            elif name == "v":
+                o[0, t:, h, c] = S[0, h, :, c] = dq[0, t:, h] = dk[0, t, h] = True
+            else:
+                dq[0, t, h] = dk[0, :t + 1, h] = dv[0, :t + 1, h, c] = dS[0, h, :, c] = True
+            for n, (got, y, r) in enumerate(zip(run(x), want, reach)):
+                assert torch.equal(got[~r], y[~r]), (name, h, n)
+                assert not torch.isfinite(got[r]).any(), (name, h, n)
+
+
 # ---- group norm ------------------------------------------------------------------------------------------------------
 def norm_inputs(rows, C, dtype, seed, mean=0.0):
     g = torch.Generator(device="cuda").manual_seed(seed)
