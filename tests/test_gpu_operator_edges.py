@@ -1,5 +1,5 @@
 """Calls of the operators beside the recurrence that their documentation allows and that are easy to get wrong: inputs that share an
-address, parameters that are not finite, groups of one value, named streams."""
+address, values and parameters that are extreme or not finite, groups of one value, named streams, waits that run out."""
 import numpy as np
 import pytest
 import torch
@@ -44,6 +44,26 @@ def test_linear_inputs_may_be_views_of_one_buffer(pair, d_k, d_v, dtype):
 
     for name, a, b in zip(("o", "S_T", "dq", "dk", "dv", "dS0"), run(views), run(alone)):
         assert torch.equal(a, b), name
+
+
+@pytest.mark.parametrize("d_k,d_v", [(64, 64), (128, 128)])
+def test_linear_fp32_keeps_the_bits_of_its_operands(d_k, d_v):
+    """Root mean squares, relative: an operand's low tf32 part (2^-11 of it at most, 2^-12.2 in the mean) is cut at 2^-10 of itself, so 1e-7 for
+    each of two operands; a product of two low parts that is left out, 4e-8; sums in accumulators, cut off at each of up to 16 steps
+    by half a unit on average, at most 16 x 2^-25 = 5e-7 where all steps are of full size, half of that on the way to it.  Two
+    products in a row: under 6e-7, and 1e-6 with the fp32 additions and powers around them."""
+    B, T, H = 1, 700, 4
+    g = torch.Generator(device="cuda").manual_seed(9)
+    r = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    q, k, v, d_o, S0, dS = r(B, T, H, d_k), r(B, T, H, d_k), r(B, T, H, d_v), r(B, T, H, d_v), r(B, H, d_k, d_v), r(B, H, d_k, d_v)
+    ld = torch.tensor([-1.0, -0.05, -2.0 ** -8, -2.0 ** -12], device="cuda")
+    o, S, grads = torch.empty_like(v), torch.empty_like(S0), [torch.empty_like(t) for t in (q, k, v, S0)]
+    sfda.sfda_linear_forward(q, k, v, ld, None, S0, o, S, 0.5)
+    sfda.sfda_linear_backward(q, k, v, ld, None, S0, d_o, dS, *grads, 0.5)
+    f = lambda t: t.double().cpu().numpy()  # noqa: E731
+    want = (*op.linear_forward(f(q), f(k), f(v), f(ld), None, f(S0), 0.5), *op.linear_backward(f(q), f(k), f(v), f(ld), f(d_o), f(dS), None, f(S0), 0.5))
+    for name, got, y in zip(("o", "S_T", "dq", "dk", "dv", "dS0"), [o, S] + grads, want):
+        assert np.linalg.norm(f(got) - y) <= 1e-6 * np.linalg.norm(y), name
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
