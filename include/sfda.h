@@ -553,7 +553,7 @@ SFDA_API int sfda_backward_withheld_handoff(const void *q, const void *k, const 
  * SFDA_BF16: chunks of 128 tokens on tcgen05.  The masked scores and a copy of the state are rounded to bf16 as operands of the
  * products that make an output (each as the output itself is); what goes into the state is in two bf16 parts, so that states
  * are about 4e-6 (relative, in the 2-norm) off.  For heads with gamma >= 0.805 scores are scaled by up to 2^40 before the row's power
- * of gamma takes that back, so |q . k| has to stay below 3e26.  With few sequences each is cut into stretches of time, whose
+ * of gamma takes that back, so |q . k| and sums of |(q . k) v| have to stay below 3e26.  With few sequences each is cut into stretches of time, whose
  * states a first launch makes (the workspace holds them).  The workspace begins with the status word that sfda_workspace_status
  * reads: every wait inside the kernel is bounded (seconds), and where one runs out the call's outputs are invalid and the status is
  * SFDA_ERR_TIMEOUT.  No CTA waits for another one.
@@ -568,8 +568,9 @@ SFDA_API int sfda_linear_forward(const void *q, const void *k, const void *v, co
 
 /*
  * Its gradients: of a real loss, given the cotangents d_o [B][T][H][d_v] dtype of the outputs and dS_T [B][H][d_k][d_v]
- * float of the final state (or NULL: zero).  With G_t = gamma_h G_{t+1} + scale q_t d_o_t^T and G behind the last token
- * = dS_T:  dq_t = scale S_t d_o_t,  dk_t = G_t v_t,  dv_t = G_t^T k_t,  dS0 = gamma_h G_1.
+ * float of the final state (or NULL: zero).  With G_n = dS_T + scale q_n d_o_n^T at a sequence's last token n, and
+ * G_t = gamma_h G_{t+1} + scale q_t d_o_t^T before it:  dq_t = scale S_t d_o_t,  dk_t = G_t v_t,  dv_t = G_t^T k_t,
+ * dS0 = gamma_h G_1 (dS_T itself for a sequence of no tokens).
  *
  *  dq [B][T][H][d_k], dk [B][T][H_kv][d_k], dv [B][T][H_kv][d_v] dtype (those of shared heads are sums over the query heads
  *  that read them, added in fp32 in a fixed order and rounded once);  dS0 [B][H][d_k][d_v] float.  All four are required
@@ -637,8 +638,8 @@ SFDA_API int sfda_rotary_turns(uint64_t *turns, int rot, double base, int scalin
  *  x, gate, y [rows][C] dtype (gate may be NULL)     weight, bias [C] float, or NULL (1 and 0)
  *  act       SFDA_ACT_NONE: the identity; SFDA_ACT_SILU: u / (1 + exp(-u))
  *  y may be x or gate.  mean and var (divided by C / G) are those of the row's group alone, so rows are independent: tokens of
- *  a causal model.  Any G that divides C; SFDA_ERR_UNSUPPORTED where
- *  groups of more than a thousand channels are more than 65535.  SFDA_ERR_VALUE unless eps is positive and finite.
+ *  a causal model.  Any G up to 65535 that divides C, and more of them (up to 16.7 M) the narrower they are;
+ *  SFDA_ERR_UNSUPPORTED beyond.  SFDA_ERR_VALUE unless eps is positive and finite.
  *
  * sfda_group_norm_backward: the gradients from dy [rows][C] dtype:  dx, dgate [rows][C] dtype (dgate is required with a
  * gate and ignored without), dweight, dbias [C] float, either of which may be NULL.  dx may be dy, dgate may be gate.

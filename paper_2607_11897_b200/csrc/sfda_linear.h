@@ -21,7 +21,7 @@ namespace sfda {
 // the first of them leaves at the front is dS0.
 struct LinearPass {
     const void *a, *b, *c;      // [B][T][Ha][DA], [B][T][Hb][DA], [B][T][Hc][DC]; head h reads head h / (H / Hx)
-    void *out;                  // [B][T][H][DC], in the dtype of the call, or float with out_f32; NULL: states only
+    void *out;                  // [B][T][H][DC], in the dtype of the call, or float with out_f32
     const float *s_in;          // [B][H][DA][DC] ([DC][DA] with s_in_t), or NULL for zero
     float *s_out;               // [B][H][DA][DC], or NULL
     int Ha, Hb, Hc, DA, DC;

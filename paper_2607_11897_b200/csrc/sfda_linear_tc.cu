@@ -17,7 +17,7 @@
 // MMA, output copies, one idle, eight each for P and the output, for the state and for w o b.  Two stages of b and c; one place for a,
 // loaded out of L2 as soon as a S is done with it; one for the output.  Measured 457 us (4.7 TB/s) in bursts and 538 us under
 // sustained load, when the clock falls: the chain P, P c, output of a chunk (5000 cycles) and the issue of its 10500 warp
-// instructions are what is left above memory.  Before: outputs stored by the warps themselves 841 us (32 rows of a warp lie in 32
+// instructions are what is left above memory, and that 256 equal chains make two waves of 148 SMs.  Before: outputs stored by the warps themselves 841 us (32 rows of a warp lie in 32
 // lines), descriptors computed per instruction 668, w o b through shared memory 562 (its bandwidth is what the products compete for).
 #include <cuda.h>
 #include <stdlib.h>
@@ -940,8 +940,9 @@ cudaError_t launch_one(Params &p, cudaStream_t stream, int *launches)
 // How many stretches each sequence is cut into, for `chains` of `chunks` chunks on n SMs: the least of a sum of measured times in
 // microseconds.  A CTA takes kChunk for a chunk (kStates for one of the pass that only makes states) and kStart for a unit; a
 // stretch reads the states of those before it, kCarry each; a second launch costs kLaunch; and memory takes kMemory for a chunk.
-// (Measured: one sequence of 131072 tokens and 16 heads 2850 us uncut, 720 in 8; 4 x 4096 and 16 heads 115 uncut, 108 in 2; 1024
-// and 8 heads 32 uncut, 39 in 2.)
+// (Measured at d = 128, replayed from a graph: one sequence of 131072 tokens and 16 heads 2883 us uncut, 733 in 8, 726 in 9; 4 x 4096
+// and 16 heads 131 uncut, 126 in 2; 4096 and 32 heads 100 uncut, 71 in 4; 1024 and 8 heads 32 uncut, 38 in 2.  The constants are those
+// of d = 128; at d = 64 the same four: 489 in 9 (473 in 18); 87 uncut, 76 in 2; 44 in 4; 23 uncut, 19 in 8.)
 static int stretches(long long chains, int chunks, int n)
 {
     constexpr double kChunk = 2.9, kStates = 2.6, kStart = 8.0, kCarry = 2.5, kLaunch = 4.0, kMemory = 0.026;
