@@ -553,10 +553,10 @@ SFDA_API int sfda_backward_withheld_handoff(const void *q, const void *k, const 
  * SFDA_BF16: chunks of 128 tokens on tcgen05.  The masked scores and a copy of the state are rounded to bf16 as operands of the
  * products that make an output (each as the output itself is); what goes into the state is in two bf16 parts, so that states
  * are about 4e-6 (relative, in the 2-norm) off.  For heads with gamma >= 0.805 scores are scaled by up to 2^40 before the row's power
- * of gamma takes that back, so |q . k| and sums of |(q . k) v| have to stay below 3e26.  With few sequences each is cut into stretches of time, whose
- * states a first launch makes (the workspace holds them).  The workspace begins with the status word that sfda_workspace_status
- * reads: every wait inside the kernel is bounded (seconds), and where one runs out the call's outputs are invalid and the status is
- * SFDA_ERR_TIMEOUT.  No CTA waits for another one.
+ * of gamma takes that back, so |q . k| and sums of |(q . k) v| have to stay below 3e26.  With few sequences each is cut
+ * into stretches of time, whose states a first launch makes (the workspace holds them).  The workspace begins with the
+ * status word that sfda_workspace_status reads: every wait inside the kernel is bounded (seconds), and where one runs
+ * out the call's outputs are invalid and the status is SFDA_ERR_TIMEOUT.  No CTA waits for another one.
  * SFDA_F32: chunks of 64 tokens, operands in two tf32 parts (22 bits), magnitudes from 2^128 - 2^116 on as if they were not
  * finite; no waits, no status word, and a workspace only for the gradients of shared heads.
  */

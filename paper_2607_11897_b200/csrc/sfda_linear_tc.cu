@@ -17,8 +17,9 @@
 // MMA, output copies, one idle, eight each for P and the output, for the state and for w o b.  Two stages of b and c; one place for a,
 // loaded out of L2 as soon as a S is done with it; one for the output.  Measured 457 us (4.7 TB/s) in bursts and 538 us under
 // sustained load, when the clock falls: the chain P, P c, output of a chunk (5000 cycles) and the issue of its 10500 warp
-// instructions are what is left above memory, and that 256 equal chains make two waves of 148 SMs.  Before: outputs stored by the warps themselves 841 us (32 rows of a warp lie in 32
-// lines), descriptors computed per instruction 668, w o b through shared memory 562 (its bandwidth is what the products compete for).
+// instructions are what is left above memory, and that 256 equal chains make two waves of 148 SMs.  Before: outputs stored by the
+// warps themselves 841 us (32 rows of a warp lie in 32 lines), descriptors computed per instruction 668, w o b through shared
+// memory 562 (its bandwidth is what the products compete for).
 #include <cuda.h>
 #include <stdlib.h>
 
